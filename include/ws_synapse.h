@@ -58,6 +58,9 @@ typedef enum {
     WS_OP_ATTENTION_MASS = 4,  /* H = G*Hkv heads, Hq = query heads per group times G */
     WS_OP_DENSITY_APPEND = 5,  /* k = m appended rows */
     WS_OP_INJECT = 6,          /* k = m injected rows */
+    WS_OP_PAGED_ATTEND = 7,    /* H = KV heads, L = rows a sequence has room for (per_seq * page), N = sequences, Hq; k = 1 with
+                                * the rows' weights (mass_out), 0 without */
+    WS_OP_PAGED_EVICT = 8,     /* H = KV heads, L and N as above, k = rows to keep */
     WS_OP_INT_RANGE = 0x7fffffff
 } ws_op;
 
@@ -317,6 +320,98 @@ ws_status ws_synapse_gate(const void *h_main, const void *T, ws_dtype dt, int N,
 ws_status ws_synapse_inject(void *Kc, void *Vc, ws_dtype dt, int H, int Lcap, int d, int L,
                             const void *Knew, const void *Vnew, int m, const int32_t *pos, float base,
                             void *workspace, size_t workspace_bytes, ws_stream stream);
+
+/* ------------------------------------------------------------------------------------------
+ * A cache in pages: the agents' own decode step, beside the synapse they share.
+ *
+ * A side agent that reads the synapse also grows a context of its own, and the main agent reads its whole context at every token.
+ * The three calls below are that step over caches whose rows lie in pages of a common pool, so that they grow without being moved:
+ * the new token's rows join the pages (keys and queries rotated to their positions), the token attends over all rows of its
+ * sequence, each row's share of the attention is added to its account, and now and then the rows with the least on their account
+ * are given up ("Attention Score Summation", Sec. 3.3, kept up while decoding).  Pages may be shared between sequences as long as
+ * none of the rows in them is written or moved: the synapse of ws_synapse_gather, put into pages once (ws_synapse_paged_append
+ * without positions), can be the head of every agent's table and is protected by `sinks` of ws_synapse_paged_evict.
+ * ------------------------------------------------------------------------------------------ */
+
+/*
+ * Row r of sequence s is row r % page of page table[s, r / page].  The structure lives on the host and is read during the call;
+ * what it points to lives on the device.
+ *   len counts what is there AFTER an append.  A value outside [0, per_seq * page] is clamped into range, a page number outside
+ *   [0, pages) is not followed: an append or a move to such a page is left out, a row read from one counts as row of page 0.
+ *   Table entries behind a sequence's last page in use are not read.  Rows behind a sequence's last one may hold anything (NaN too).
+ */
+typedef struct {
+    void *K, *V;              /* dev [pages, Hkv, page, d] each, 16-byte aligned */
+    const int32_t *table;     /* dev [S, per_seq] page numbers */
+    const int32_t *len;       /* dev [S] rows in use */
+    ws_dtype dt;
+    int pages, Hkv, page, d;  /* page: 16, 32, 64, 128 or 256 rows; d: 64 or 128 */
+    int S, per_seq;           /* per_seq * page < 2^24 */
+} ws_paged_cache;
+
+/* Rows of new tokens, wherever a projection left them: element e of head h of token t is x[t * token + h * head + e].  Strides count
+ * elements, are not negative and multiples of 16 bytes; x is 16-byte aligned. */
+typedef struct {
+    const void *x;
+    int64_t token, head;
+} ws_rows;
+
+/*
+ * The rows of T new tokens join the cache, rotated to their positions, and the tokens' queries are rotated with them.
+ * Token t belongs to the sequence s with first[s] <= t < first[s+1]; with n = first[s+1] - first[s] it becomes row
+ * len[s] - n + (t - first[s]) of s (len: after the append).  Rotation of a row x of d elements, pairs (c, c + d/2):
+ *     a = pos[axis(c), t] * base^(-2c/d),   y_c = x_c cos a - x_{c+d/2} sin a,   y_{c+d/2} = x_{c+d/2} cos a + x_c sin a
+ * where axis(c) counts the pairs off: the first pairs_host[0] pairs go by axis 0, the next pairs_host[1] by axis 1, ... (one axis:
+ * text; three: time, height, width of images and video).  Products of position and frequency are formed in float64 and reduced
+ * before the fp32 sine and cosine; a rotated row is rounded once.
+ *   k, v       rows [T, Hkv, d] of the new tokens, dtype of the cache
+ *   first      dev [S+1], first[0] = 0, not falling; tokens t >= first[S] are left out (a padded batch)
+ *   pos        dev [axes, T] positions, or NULL: keys and queries are copied as they are (axes, pairs_host, base are not looked at)
+ *   axes       1 to 4;  pairs_host host [axes] numbers of pairs, each >= 0, d/2 in all;  base > 0
+ *   q, q_out   rows [T, Hq, d] and dev [T, Hq, d] dense, written; q NULL: keys and values only (Hq and q_out are not looked at)
+ *   stamp      dev [S, Hkv, per_seq * page] int32 or NULL: the new rows' numbers in the order of their sequence,
+ *              seen[s] - n + (t - first[s]), which stay with a row when an eviction moves it
+ *   seen       dev [S] tokens the sequence has had so far, this append included (len while nothing was evicted); NULL with stamp NULL
+ *   mass       dev [S, Hkv, per_seq * page] fp32 or NULL: the new rows' accounts, set to 0
+ * A new row must not be shared between sequences, and q_out must not overlap k, v or q.  Rows outside the table are left out.
+ */
+ws_status ws_synapse_paged_append(const ws_paged_cache *cache, const ws_rows *k, const ws_rows *v, int T, const int32_t *first,
+                                  const int32_t *pos, int axes, const int *pairs_host, float base, const ws_rows *q, int Hq,
+                                  void *q_out, const int32_t *seen, int32_t *stamp, float *mass, ws_stream stream);
+
+/*
+ * Attention of one new token of every sequence over all rows of its cache:
+ *     O[s,q,:] = sum_r p[q,r] V[s,q/g,r,:],   p[q,:] = softmax_r( scale * Q[s,q,:] . K[s,q/g,r,:] ),   g = Hq/Hkv,  r < len[s]
+ *     lse[s,q] = ln sum_r exp( scale * Q[s,q,:] . K[s,q/g,r,:] )
+ *     mass_out[s,h,r] = decay * mass_in[s,h,r] + sum_{q in the g heads of h} p[q,r]                         r < len[s]
+ * A sequence of no rows gives O = 0 and lse = -infinity.  The cache is split over the device by its rows, whatever their
+ * sequence, and joined; the same call on the same device gives the same bits.
+ *   Q dev [S, Hq, d] dtype of the cache, already rotated;  Hq % Hkv == 0;  scale <= 0 means 1/sqrt(d)
+ *   O dev [S, Hq, d] fp32;  lse dev [S, Hq] fp32 or NULL
+ *   mass_out dev [S, Hkv, per_seq * page] fp32 or NULL: no weights;  mass_in the same or NULL: from 0 on;  mass_in may be mass_out.
+ *   Entries of rows behind len[s] are left as they are.  decay finite, >= 0 (1: a plain sum).
+ *   The accounts are kept by sequence, not by page, so sequences that share pages have accounts of their own.
+ */
+ws_status ws_synapse_paged_attend(const ws_paged_cache *cache, const void *Q, int Hq, float scale, float *O, float *lse, float decay,
+                                  const float *mass_in, float *mass_out, void *workspace, size_t workspace_bytes, ws_stream stream);
+
+/*
+ * Every KV head of every sequence with more than `keep` rows gives up the ones with the least on their account, down to `keep`.
+ * Rows with stamp < sinks or stamp >= seen[s] - recent are protected and stay; of the others those with the largest mass stay, of
+ * equal ones those in the lowest row (a NaN counts as the least).  Stays that lie in the first `keep` rows are not moved; the
+ * others fill the rows that became free below `keep`, in order: the i-th of them goes to the i-th free row.  (Attention does not
+ * depend on the rows' order; moving no more than this is what the stamps are for.)  K, V, mass and stamp move together.
+ *   seen      dev [S] as for the append;  sinks, recent >= 0, sinks + recent <= keep, keep >= 1
+ *   mass_in, stamp_in    dev [S, Hkv, per_seq * page]
+ *   mass_out, stamp_out  the same, entries below len_out[s] written, the others left as they are; either may be its input
+ *   len_out   dev [S], min(len, keep), written; may be cache->len
+ *   kept      dev [S, Hkv, keep] int32 or NULL: the row each row below len_out[s] was before (entries behind left as they are)
+ * Rows of K and V at `keep` and behind are left as they are, so the call can be made again with the same inputs.  A page in which rows
+ * move must not be shared between sequences; rows that are protected from the first eviction on, at the head of the table, never move.
+ */
+ws_status ws_synapse_paged_evict(const ws_paged_cache *cache, int keep, int sinks, int recent, const int32_t *seen,
+                                 const float *mass_in, float *mass_out, const int32_t *stamp_in, int32_t *stamp_out,
+                                 int32_t *len_out, int32_t *kept, void *workspace, size_t workspace_bytes, ws_stream stream);
 
 /* Whether bf16 heads of these sizes stay on chip for all steps on the current device where ws_synapse_select_is_lazy says 0:
  * 1 = they do (the resident or the one-workgroup kernel), 0 = streaming.  0 for fp32 keys, also where the

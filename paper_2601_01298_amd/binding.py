@@ -16,6 +16,7 @@ WS_OK, WS_ERR_INVALID_ARG, WS_ERR_UNSUPPORTED, WS_ERR_WORKSPACE, WS_ERR_HIP, WS_
 WS_F32, WS_BF16 = 0, 1
 WS_OP_DENSITY, WS_OP_SELECT, WS_OP_GATHER, WS_OP_ATTEND = range(4)
 WS_OP_ATTENTION_MASS, WS_OP_DENSITY_APPEND, WS_OP_INJECT = 4, 5, 6
+WS_OP_PAGED_ATTEND, WS_OP_PAGED_EVICT = 7, 8
 WS_SELECT_AUTO, WS_SELECT_STREAMING, WS_SELECT_RESIDENT = 0, 1, 2
 _SELECT_KERNELS = {"auto": WS_SELECT_AUTO, "stream": WS_SELECT_STREAMING, "resident": WS_SELECT_RESIDENT}
 
@@ -28,6 +29,17 @@ class SelectPlan(ctypes.Structure):
     """Mirror of ws_select_plan."""
     _fields_ = [(n, ctypes.c_int) for n in ("resident", "heads_in_flight", "workgroups_per_head", "threads",
                                             "rows_in_registers", "rows_in_lds", "compute_units")]
+
+
+class _PagedCache(ctypes.Structure):
+    """Mirror of ws_paged_cache."""
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("table", ctypes.c_void_p), ("len", ctypes.c_void_p),
+                *((n, ctypes.c_int) for n in ("dt", "pages", "Hkv", "page", "d", "S", "per_seq"))]
+
+
+class _Rows(ctypes.Structure):
+    """Mirror of ws_rows."""
+    _fields_ = [("x", ctypes.c_void_p), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
 
 
 class WsError(RuntimeError):
@@ -78,6 +90,13 @@ def lib() -> ctypes.CDLL:
         L.ws_synapse_gate.restype = ci
         L.ws_synapse_inject.argtypes = [vp, vp, ci, ci, ci, ci, ci, vp, vp, ci, vp, cf, vp, sz, vp]
         L.ws_synapse_inject.restype = ci
+        paged, rows = ctypes.POINTER(_PagedCache), ctypes.POINTER(_Rows)
+        L.ws_synapse_paged_append.argtypes = [paged, rows, rows, ci, vp, vp, ci, ctypes.POINTER(ci), cf, rows, ci, vp, vp, vp, vp, vp]
+        L.ws_synapse_paged_append.restype = ci
+        L.ws_synapse_paged_attend.argtypes = [paged, vp, ci, cf, vp, vp, cf, vp, vp, vp, sz, vp]
+        L.ws_synapse_paged_attend.restype = ci
+        L.ws_synapse_paged_evict.argtypes = [paged, ci, ci, ci, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.ws_synapse_paged_evict.restype = ci
         L.ws_synapse_select_is_resident.argtypes = [ci, ci, ci, ci]
         L.ws_synapse_select_is_resident.restype = ci
         L.ws_synapse_select_is_lazy.argtypes = [ci, ci, ci, ci, ci]
@@ -428,3 +447,168 @@ def ws_synapse_inject(Kc: torch.Tensor, Vc: torch.Tensor, L: int, Knew: torch.Te
                                    m, pos.data_ptr(), float(base), workspace.data_ptr(), workspace.numel(),
                                    _stream(stream)), "ws_synapse_inject")
     return L + m
+
+
+class PagedCache:
+    """Pools K, V [pages, Hkv, page, d], table [S, per_seq] int32 page numbers, len [S] int32 rows in use: what the calls
+    below work on.  The tensors stay the caller's; make a new PagedCache when one of them is replaced."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, len: torch.Tensor):
+        _dev(K, "K")
+        if K.dim() != 4:
+            raise ValueError("K must be [pages, Hkv, page, d]")
+        _want(V, "V", K.shape, K.dtype)
+        if table.dim() != 2:
+            raise ValueError("table must be [S, per_seq]")
+        _want(table, "table", table.shape, torch.int32)
+        _want(len, "len", (table.shape[0],), torch.int32)
+        self.K, self.V, self.table, self.len = K, V, table, len
+        self.pages, self.Hkv, self.page, self.d = K.shape
+        self.S, self.per_seq = table.shape
+        self.rows = self.per_seq * self.page
+        self.device = K.device
+        for t, name in ((V, "V"), (table, "table"), (len, "len")):
+            self._here(t, name)
+        self._c = _PagedCache(K.data_ptr(), V.data_ptr(), table.data_ptr(), len.data_ptr(), _dtype_code(K), self.pages, self.Hkv,
+                              self.page, self.d, self.S, self.per_seq)
+
+    def _here(self, t: torch.Tensor, name: str):
+        if t.device != self.device:
+            raise ValueError(f"{name} must be on the cache's device, {self.device}, not on {t.device}")
+
+    def _want(self, t: torch.Tensor, name: str, shape, dtype) -> torch.Tensor:
+        _want(t, name, shape, dtype)
+        self._here(t, name)
+        return t
+
+    def _rows(self, t: torch.Tensor, name: str, T: int, heads: int) -> _Rows:
+        """Rows [T, heads, d] of any strides over whole rows."""
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a device tensor")
+        self._here(t, name)
+        if t.dtype != self.K.dtype:
+            raise TypeError(f"{name} must be {self.K.dtype}, got {t.dtype}")
+        if tuple(t.shape) != (T, heads, self.d):
+            raise ValueError(f"{name} must have shape {(T, heads, self.d)}, got {tuple(t.shape)}")
+        token, head, element = t.stride()
+        if element != 1:
+            raise ValueError(f"the elements of a row of {name} must be contiguous")
+        return _Rows(t.data_ptr(), token, head)
+
+    def _stream(self, stream) -> int:
+        """The stream to enqueue on; kernels are launched on the current device, so the cache has to be there."""
+        if self.device.index != torch.cuda.current_device():
+            raise ValueError(f"the cache is on {self.device}, the current device is {torch.cuda.current_device()}")
+        return _stream(stream)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def ws_synapse_paged_workspace(cache: PagedCache, op: str, Hq: int = 0, weights: bool = False, keep: int = 0, stream=None) -> torch.Tensor:
+    """A workspace for op "attend" (Hq query heads, with or without the rows' weights) or "evict" (keep rows)."""
+    dt = _dtype_code(cache.K)
+    if op == "attend":
+        n = ws_synapse_workspace_bytes(WS_OP_PAGED_ATTEND, dt, cache.Hkv, cache.rows, cache.d, k=int(weights), N=cache.S, Hq=Hq)
+    elif op == "evict":
+        n = ws_synapse_workspace_bytes(WS_OP_PAGED_EVICT, dt, cache.Hkv, cache.rows, cache.d, k=keep, N=cache.S)
+    else:
+        raise ValueError(f"no workspace for {op!r}")
+    return _workspace(n, cache.device, None, stream)
+
+
+def ws_synapse_paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, first: torch.Tensor, pos: torch.Tensor | None = None,
+                            pairs=None, base: float = 1e6, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
+                            seen: torch.Tensor | None = None, stamp: torch.Tensor | None = None, mass: torch.Tensor | None = None,
+                            stream=None):
+    """k, v [T,Hkv,d] (any strides over rows) join the cache, whose len already counts them; first [S+1] int32.
+    pos [axes,T] (or [T]) int32 and pairs (d/2 pairs for one axis): keys rotate, and q [T,Hq,d] into q_out, which is returned.
+    stamp [S,Hkv,rows] int32 (with seen [S] int32) and mass [S,Hkv,rows] fp32 are started for the new rows."""
+    T = k.shape[0]
+    krows, vrows = cache._rows(k, "k", T, cache.Hkv), cache._rows(v, "v", T, cache.Hkv)
+    cache._want(first, "first", (cache.S + 1,), torch.int32)
+    axes, npairs = 0, None
+    if pos is not None:
+        axes = 1 if pos.dim() == 1 else pos.shape[0]
+        cache._want(pos, "pos", (T,) if pos.dim() == 1 else (axes, T), torch.int32)
+        pairs = [cache.d // 2] if pairs is None and axes == 1 else list(pairs or ())
+        if len(pairs) != axes:
+            raise ValueError("one number of pairs per axis")
+        npairs = (ctypes.c_int * axes)(*[int(n) for n in pairs])
+    qrows, Hq = None, 0
+    if q is not None:
+        if q.dim() != 3:
+            raise ValueError("q must be [T,Hq,d]")
+        Hq = q.shape[1]
+        qrows = cache._rows(q, "q", T, Hq)
+        if q_out is None:
+            q_out = _new((T, Hq, cache.d), q.dtype, cache.device, stream)
+        cache._want(q_out, "q_out", (T, Hq, cache.d), q.dtype)
+    shape = (cache.S, cache.Hkv, cache.rows)
+    if seen is not None:
+        cache._want(seen, "seen", (cache.S,), torch.int32)
+    if stamp is not None:
+        cache._want(stamp, "stamp", shape, torch.int32)
+    if mass is not None:
+        cache._want(mass, "mass", shape, torch.float32)
+    _check(lib().ws_synapse_paged_append(ctypes.byref(cache._c), ctypes.byref(krows), ctypes.byref(vrows), T, first.data_ptr(), _ptr(pos),
+                                         axes, npairs, float(base), None if qrows is None else ctypes.byref(qrows), Hq,
+                                         _ptr(q_out) if q is not None else None, _ptr(seen), _ptr(stamp), _ptr(mass),
+                                         cache._stream(stream)), "ws_synapse_paged_append")
+    return q_out
+
+
+def ws_synapse_paged_attend(cache: PagedCache, Q: torch.Tensor, scale: float = 0.0, O: torch.Tensor | None = None,
+                            lse: torch.Tensor | None = None, decay: float = 1.0, mass_in: torch.Tensor | None = None,
+                            mass_out: torch.Tensor | None = None, workspace=None, stream=None):
+    """Q [S,Hq,d], one token of every sequence -> O [S,Hq,d] fp32; lse [S,Hq] fp32 if given.
+    mass_out [S,Hkv,rows] fp32 if given: decay * mass_in (None: 0) plus the weight each row received."""
+    if Q.dim() != 3:
+        raise ValueError("Q must be [S,Hq,d]")
+    Hq = Q.shape[1]
+    cache._want(Q, "Q", (cache.S, Hq, cache.d), cache.K.dtype)
+    if O is None:
+        O = _new((cache.S, Hq, cache.d), torch.float32, cache.device, stream)
+    cache._want(O, "O", (cache.S, Hq, cache.d), torch.float32)
+    if lse is not None:
+        cache._want(lse, "lse", (cache.S, Hq), torch.float32)
+    shape = (cache.S, cache.Hkv, cache.rows)
+    if mass_in is not None:
+        cache._want(mass_in, "mass_in", shape, torch.float32)
+    if mass_out is not None:
+        cache._want(mass_out, "mass_out", shape, torch.float32)
+    if workspace is None:
+        workspace = ws_synapse_paged_workspace(cache, "attend", Hq, mass_out is not None, stream=stream)
+    else:
+        workspace = _workspace(0, cache.device, workspace)
+        cache._here(workspace, "workspace")
+    _check(lib().ws_synapse_paged_attend(ctypes.byref(cache._c), Q.data_ptr(), Hq, float(scale), O.data_ptr(), _ptr(lse), float(decay),
+                                         _ptr(mass_in), _ptr(mass_out), workspace.data_ptr(), workspace.nbytes,
+                                         cache._stream(stream)), "ws_synapse_paged_attend")
+    return O
+
+
+def ws_synapse_paged_evict(cache: PagedCache, keep: int, seen: torch.Tensor, mass_in: torch.Tensor, stamp_in: torch.Tensor,
+                           sinks: int = 0, recent: int = 0, mass_out: torch.Tensor | None = None, stamp_out: torch.Tensor | None = None,
+                           len_out: torch.Tensor | None = None, kept: torch.Tensor | None = None, workspace=None, stream=None):
+    """Every sequence is cut to `keep` rows per KV head: the protected ones and those with the largest mass.  K and V move in
+    place; mass, stamp [S,Hkv,rows] and len [S] too, unless mass_out, stamp_out, len_out are given.  Returns len_out."""
+    shape = (cache.S, cache.Hkv, cache.rows)
+    cache._want(seen, "seen", (cache.S,), torch.int32)
+    cache._want(mass_in, "mass_in", shape, torch.float32)
+    cache._want(stamp_in, "stamp_in", shape, torch.int32)
+    mass_out = mass_in if mass_out is None else cache._want(mass_out, "mass_out", shape, torch.float32)
+    stamp_out = stamp_in if stamp_out is None else cache._want(stamp_out, "stamp_out", shape, torch.int32)
+    len_out = cache.len if len_out is None else cache._want(len_out, "len_out", (cache.S,), torch.int32)
+    if kept is not None:
+        cache._want(kept, "kept", (cache.S, cache.Hkv, keep), torch.int32)
+    if workspace is None:
+        workspace = ws_synapse_paged_workspace(cache, "evict", keep=keep, stream=stream)
+    else:
+        workspace = _workspace(0, cache.device, workspace)
+        cache._here(workspace, "workspace")
+    _check(lib().ws_synapse_paged_evict(ctypes.byref(cache._c), int(keep), int(sinks), int(recent), seen.data_ptr(), mass_in.data_ptr(),
+                                        mass_out.data_ptr(), stamp_in.data_ptr(), stamp_out.data_ptr(), len_out.data_ptr(), _ptr(kept),
+                                        workspace.data_ptr(), workspace.nbytes, cache._stream(stream)), "ws_synapse_paged_evict")
+    return len_out
