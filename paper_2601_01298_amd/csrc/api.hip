@@ -61,8 +61,10 @@ size_t ws_synapse_workspace_bytes(ws_op op, ws_dtype dt, int H, int L, int d, in
         return ws::inject_workspace_bytes(d, k);
     case WS_OP_PAGED_ATTEND:
         // H = KV heads, Hq = query heads, L = rows a sequence has room for, N = sequences, k != 0: with the rows' weights
-        if (H < 1 || Hq < 1 || N < 1 || L < 1 || L >= kMaxL || Hq % H != 0 || (long long)N * Hq > (1 << 20)) return (size_t)-1;
-        return ws::paged_attend_workspace_bytes(N, H, Hq, L, d, k != 0);
+        if (H < 1 || Hq < 1 || N < 1 || L < 1 || L >= kMaxL || Hq % H != 0 || (long long)N * Hq > (1 << 20) ||
+            ws::paged_most_tiles(dt == WS_BF16, N, H, Hq, L) > 0x7FFFFFFFLL)
+            return (size_t)-1;
+        return ws::paged_attend_workspace_bytes(dt == WS_BF16, N, H, Hq, L, d, k != 0);
     case WS_OP_PAGED_EVICT:
         if (H < 1 || N < 1 || L < 1 || L >= kMaxL || k < 1 || (long long)N * H > (1 << 20)) return (size_t)-1;
         return ws::paged_evict_workspace_bytes(N, H, L, k);

@@ -85,7 +85,9 @@ ws_status ws_synapse_paged_attend(const ws_paged_cache *cache, const void *Q, in
     if (mass_out && !(decay >= 0.0f && std::isfinite(decay))) return WS_ERR_INVALID_ARG;
     if ((long long)cache->S * Hq > (1 << 20)) return WS_ERR_UNSUPPORTED;
     const int cap = cache->per_seq * cache->page;
-    s = check_ws(workspace, workspace_bytes, ws::paged_attend_workspace_bytes(cache->S, cache->Hkv, Hq, cap, cache->d, mass_out != nullptr));
+    const bool bf16 = cache->dt == WS_BF16;
+    if (ws::paged_most_tiles(bf16, cache->S, cache->Hkv, Hq, cap) > 0x7FFFFFFFLL) return WS_ERR_UNSUPPORTED;
+    s = check_ws(workspace, workspace_bytes, ws::paged_attend_workspace_bytes(bf16, cache->S, cache->Hkv, Hq, cap, cache->d, mass_out != nullptr));
     if (s != WS_OK) return s;
     if (scale <= 0.0f) scale = 1.0f / std::sqrt((float)cache->d);
     const hipError_t e = ws::launch_paged_attend(*cache, Q, Hq, scale, O, lse, decay, mass_in, mass_out, workspace, (hipStream_t)stream);

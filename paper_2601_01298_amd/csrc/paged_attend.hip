@@ -1,150 +1,411 @@
 // Attention of one new token of every sequence over its paged cache.
 //     z[q,r] = scale Q[q].K[r],  O[q] = sum_r exp(z - m) V[r] / sum_r exp(z - m)
 //
-// paged_split: a workgroup takes one KV head of one sequence and one of `splits` equal ranges of its rows, in tiles of 64 rows with
-// the softmax's running maximum and sum, and leaves maximum, sum and unnormalised output per query head; paged_join: one wave
-// per query head brings the splits to their common maximum; paged_weights: adds the rows' weights, from the logits that
-// paged_split left, to their accounts.  Logits are kept in units of log2.
+// paged_split reads the cache once.  The rows of all (sequence, KV head) pairs are counted off in tiles of TR rows, and every
+// workgroup takes an equal run of tiles across the borders of pairs, so that a batch of unequal lengths keeps the whole chip busy.
+// Inside its part of a pair the four waves take tiles in turn; a wave does
+//     S^T = K_tile . Q^T    (rows of the result: cache rows, columns: up to 16 query heads)
+//     O^T += V_tile^T . P^T (rows: head dimensions, columns: query heads)
+// with 16x16 matrix instructions.  Both results hold one query head per lane (lane & 15), so maximum, sum and rescaling are plain
+// per-lane arithmetic, and the weights leave the softmax in the lane and order the second product's operand wants: the order of the
+// rows within a contraction is free as long as V is fetched in the same one.  A lane's block of V is rows x head dimensions, which
+// the product wants the other way round; eight rows of bf16 are turned in registers by one byte permutation per pair.  Nothing of K, V
+// or P goes through LDS.  Bound: HBM (g flop per byte against 250).
+//
+// paged_join brings the parts of a pair that several workgroups shared to their common maximum; paged_weights adds the rows'
+// weights, from the logits that paged_split left, to their accounts.  Logits and maxima are in units of log2.
+#include <type_traits>
+
 #include "paged_internal.h"
 
 namespace ws {
 
-namespace {
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 
-constexpr int kTile = 64;
+namespace {
 
 struct AttendArgs {
     const void *K, *V, *Q;
     const int32_t *table, *len;
-    int pages, H, page, S, per_seq, Hq, splits;
+    int pages, H, page_shift, S, per_seq, Hq, tiles_q;
     float scale_log2;
-    float *partial, *stats, *logits;
+    int32_t *total, *start;                  // [1] tiles in all; [S,H,tiles_q] first tile of every pair
+    float *stats;                            // [S,Hq] log2 of the sum of all weights
+    float *slot_stats, *slots;               // [2 * groups][gt][2], [2 * groups][gt][D]
+    float *logits;                           // [S,Hq,cap] or NULL
     float *O, *lse;
     const float *mass_in;
     float *mass_out;
     float decay;
 };
 
-template <bool BF16>
-__device__ __forceinline__ float element(const void *p, long long i)
+// An equal share of `total` tiles for each of `groups`: group b's run starts at ...
+__device__ __forceinline__ int share_start(int total, int groups, int b)
 {
-    if constexpr (BF16) return __uint_as_float((uint32_t) reinterpret_cast<const uint16_t *>(p)[i] << 16);
-    else return reinterpret_cast<const float *>(p)[i];
+    const int per = total / groups, rest = total % groups;
+    return b * per + min(b, rest);
 }
-
-__device__ __forceinline__ void split_range(int n, int splits, int sp, int &r0, int &r1)
+// ... and tile t is in the run of group
+__device__ __forceinline__ int share_owner(int total, int groups, int t)
 {
-    const int per = ((n + splits - 1) / splits + kTile - 1) / kTile * kTile;
-    r0 = min(n, sp * per);
-    r1 = min(n, r0 + per);
+    const int per = total / groups, rest = total % groups;
+    return t < (per + 1) * rest ? t / (per + 1) : rest + (t - (per + 1) * rest) / per;
 }
 
 template <bool BF16, int D>
-__global__ void __launch_bounds__(256)
+struct Shape {
+    static constexpr int TR = BF16 ? 32 : 16;            // rows of a tile
+    static constexpr int RB = D * (BF16 ? 2 : 4);        // bytes of a row
+    static constexpr int HV = TR / 16;                   // 16-row halves of a tile
+    static constexpr int NK = RB / 64;                   // 16-byte loads of K per lane and half
+    static constexpr int C = D / 16;                     // head dimensions per lane: a lane's block of V is rows x C
+    static constexpr int VW = C * (BF16 ? 2 : 4) / 4;    // 32-bit words of them
+    static constexpr int NV = 4 * HV;                    // rows of V per lane
+};
+
+template <bool BF16, int D>
+struct Tile {
+    uint4 k[Shape<BF16, D>::HV][Shape<BF16, D>::NK];
+    uint32_t v[Shape<BF16, D>::NV][Shape<BF16, D>::VW];
+};
+
+template <bool BF16, int D, bool WEIGHTS>
+__global__ void __launch_bounds__(256, 3)
 paged_split(AttendArgs a)
 {
-    __shared__ float z[kTile];
-    __shared__ float part[256];
-    const int tid = threadIdx.x;
-    const int sp = blockIdx.x % a.splits, pair = blockIdx.x / a.splits;
-    const int s = pair / a.H, h = pair % a.H, g = a.Hq / a.H;
-    const int cap = a.per_seq * a.page;
-    const int n = paged_rows(a.len[s], cap);
-    int r0, r1;
-    split_range(n, a.splits, sp, r0, r1);
-    for (int j = 0; j < g; ++j) {
-        const int qh = h * g + j;
-        float m = -__builtin_inff(), l = 0.0f, acc = 0.0f;
-        for (int t0 = r0; t0 < r1; t0 += kTile) {
-            const int rows = min(kTile, r1 - t0);
-            // four threads per row
-            const int r = tid >> 2, lane = tid & 3;
-            float dot = 0.0f;
-            if (r < rows) {
-                const int row = t0 + r;
-                const long long base = paged_base(a.table[(long long)s * a.per_seq + row / a.page], a.pages, a.H, h, a.page) + row % a.page;
-                for (int e = lane; e < D; e += 4)
-                    dot = fmaf(element<BF16>(a.Q, ((long long)s * a.Hq + qh) * D + e), element<BF16>(a.K, base * D + e), dot);
+    using P = Shape<BF16, D>;
+    constexpr int TR = P::TR, RB = P::RB, HV = P::HV, NK = P::NK, C = P::C, VW = P::VW, NV = P::NV;
+    constexpr int LD = D + 4;                            // a row of the merge area: shifts the banks from query to query
+    __shared__ float red[4][kPagedQueries][LD];
+    __shared__ float red_m[4][kPagedQueries], red_l[4][kPagedQueries];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lq = lane & 15, lj = lane >> 4;
+    const int b = blockIdx.x, groups = gridDim.x;
+    const int cap = a.per_seq << a.page_shift, pmask = (1 << a.page_shift) - 1;
+    const int pairs = a.H * a.tiles_q;                   // of one sequence
+    const int g = a.Hq / a.H;
+
+    // ---- this workgroup's run of tiles, and the sequence it starts in.  Every wave finds them for itself: a lane counts the
+    // tiles of some consecutive sequences, a scan over the lanes gives the sequence's first tile.
+    const int each = (a.S + 63) / 64;
+    int mine = 0;
+    for (int i = 0; i < each; ++i) {
+        const int s = lane * each + i;
+        if (s < a.S) mine += (paged_rows(a.len[s], cap) + TR - 1) / TR;
+    }
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(upto, o);
+        if (lane >= o) upto += y;
+    }
+    const int total = __builtin_amdgcn_readlane(upto, 63) * pairs;
+    if (b == 0 && tid == 0) *a.total = total;
+    int t0 = share_start(total, groups, b);
+    const int t1 = share_start(total, groups, b + 1);
+    if (t0 >= t1) return;
+    int s, first;                                        // first tile of sequence s
+    {
+        // the first lane whose sequences reach beyond t0
+        const unsigned long long reach = __ballot((long long)upto * pairs > t0);
+        const int l = __builtin_ctzll(reach);
+        s = l * each;
+        first = (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l)) * pairs;
+        for (;;) {
+            const int ts = (paged_rows(a.len[s], cap) + TR - 1) / TR * pairs;
+            if (t0 < first + ts) break;
+            first += ts;
+            ++s;
+        }
+    }
+    const int run0 = t0;
+    while (t0 < t1) {
+        const int n = paged_rows(a.len[s], cap);
+        const int ts = (n + TR - 1) / TR;                // tiles of a pair of this sequence
+        if (ts == 0 || t0 >= first + ts * pairs) {
+            first += ts * pairs;
+            ++s;
+            continue;
+        }
+        const int pair = (t0 - first) / ts;              // head and query tile
+        const int pair0 = first + pair * ts;
+        const int ta = t0 - pair0, tb = min(ts, t1 - pair0);
+        const int h = pair / a.tiles_q, q0 = pair % a.tiles_q * kPagedQueries;
+        const int gt = min(kPagedQueries, g - q0);
+        const long long qrow = (long long)s * a.Hq + h * g + q0;
+        const int32_t *table = a.table + (long long)s * a.per_seq;
+        const int last16 = (n - 1) & ~15;                // a tile's second half may not exist: it reads this one instead
+
+        // queries: the lane's part of query lq's row, in the order of the K loads; heads that do not exist are zero
+        uint4 qf[NK];
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk) {
+            qf[kk] = make_uint4(0, 0, 0, 0);
+            if (lq < gt)
+                qf[kk] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(a.Q) + (qrow + lq) * RB + kk * 64 + lj * 16);
+        }
+        auto half_base = [&](int t, int hf) {            // where half hf of tile t starts in the pools
+            const int r = min(t * TR + 16 * hf, last16);
+            const int p = table[r >> a.page_shift];
+            return (unsigned long long)(paged_base(p, a.pages, a.H, h, 1 << a.page_shift) + (r & pmask)) * RB;
+        };
+        const int koff = lq * RB + lj * 16, voff = 4 * lj * RB + lq * VW * 4;
+        auto load_k = [&](Tile<BF16, D> &x, int t) {
+#pragma unroll
+            for (int hf = 0; hf < HV; ++hf) {
+                const char *p = reinterpret_cast<const char *>(a.K) + half_base(t, hf);
+#pragma unroll
+                for (int kk = 0; kk < NK; ++kk) x.k[hf][kk] = *reinterpret_cast<const uint4 *>(p + koff + kk * 64);
             }
-            dot = lane_group_sum<4>(dot);
-            __syncthreads();
-            if (lane == 0) z[r] = r < rows ? dot * a.scale_log2 : -__builtin_inff();
-            __syncthreads();
-            float top = m;
-            for (int i = 0; i < rows; ++i) top = fmaxf(top, z[i]);
-            const float fade = exp2f(m - top);
-            m = top;
-            if (a.logits != nullptr && tid < rows) a.logits[((long long)s * a.Hq + qh) * cap + t0 + tid] = z[tid];
-            l *= fade;
-            acc *= fade;
-            for (int i = 0; i < rows; ++i) l += exp2f(z[i] - m);
-            // 256 / D threads per output element, each every so many rows
-            for (int i = tid / D; i < rows; i += 256 / D) {
-                const int row = t0 + i;
-                const long long base = paged_base(a.table[(long long)s * a.per_seq + row / a.page], a.pages, a.H, h, a.page) + row % a.page;
-                acc = fmaf(exp2f(z[i] - m), element<BF16>(a.V, base * D + tid % D), acc);
+        };
+        auto load_v = [&](Tile<BF16, D> &x, int t) {
+#pragma unroll
+            for (int hf = 0; hf < HV; ++hf) {
+                const char *p = reinterpret_cast<const char *>(a.V) + half_base(t, hf);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t *src = reinterpret_cast<const uint32_t *>(p + voff + i * RB);
+                    if constexpr (VW == 2) {
+                        const uint2 w = *reinterpret_cast<const uint2 *>(src);
+                        x.v[4 * hf + i][0] = w.x, x.v[4 * hf + i][1] = w.y;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < VW / 4; ++j) {
+                            const uint4 w = *reinterpret_cast<const uint4 *>(src + 4 * j);
+                            x.v[4 * hf + i][4 * j] = w.x, x.v[4 * hf + i][4 * j + 1] = w.y;
+                            x.v[4 * hf + i][4 * j + 2] = w.z, x.v[4 * hf + i][4 * j + 3] = w.w;
+                        }
+                    }
+                }
             }
+        };
+
+        float m = -__builtin_inff(), l = 0.0f;           // of query lq; l of the lane's rows only
+        f32x4_t acc[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) acc[c] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+
+        Tile<BF16, D> x;
+        int t = ta + wave;
+        if (t < tb) {
+            load_k(x, t);
+            load_v(x, t);
+        }
+        for (; t < tb; t += 4) {
+            // ---- scores of rows 16 hf + 4 lj + i for query lq
+            f32x4_t z[HV];
+#pragma unroll
+            for (int hf = 0; hf < HV; ++hf) {
+                z[hf] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int kk = 0; kk < NK; ++kk) {
+                    if constexpr (BF16) {
+                        z[hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x.k[hf][kk]),
+                                                                       __builtin_bit_cast(bf16x8_t, qf[kk]), z[hf], 0, 0, 0);
+                    } else {
+                        const uint32_t kw[4] = {x.k[hf][kk].x, x.k[hf][kk].y, x.k[hf][kk].z, x.k[hf][kk].w};
+                        const uint32_t qw[4] = {qf[kk].x, qf[kk].y, qf[kk].z, qf[kk].w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            z[hf] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kw[e]), __uint_as_float(qw[e]), z[hf], 0, 0, 0);
+                    }
+                }
+            }
+            if (t + 4 < tb) load_k(x, t + 4);
+            const int r0 = t * TR + 4 * lj;              // the lane's first row
+            const bool whole = (t + 1) * TR <= n;
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int hf = 0; hf < HV; ++hf)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    z[hf][i] *= a.scale_log2;
+                    // rows behind the sequence's last one hold anything: their score is replaced, and so is their V below
+                    if (!whole && r0 + 16 * hf + i >= n) z[hf][i] = -__builtin_inff();
+                    top = fmaxf(top, z[hf][i]);
+                }
+            if (WEIGHTS && lq < gt) {
+                float *to = a.logits + (qrow + lq) * cap + r0;
+#pragma unroll
+                for (int hf = 0; hf < HV; ++hf)
+                    if (whole || r0 + 16 * hf < n) *reinterpret_cast<f32x4_t *>(to + 16 * hf) = z[hf];
+            }
+            // the reference is moved only when a score exceeds it by more than 2^8: weights stay far from overflow, and the
+            // accumulator is rescaled a few times per pass instead of once per tile.  (All four lanes of a query agree.)
+            if (__any(top > m + 8.0f)) {
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float to = fmaxf(m, top);
+                const float fade = __builtin_amdgcn_exp2f(m - to);
+                m = to;
+                l *= fade;
+#pragma unroll
+                for (int c = 0; c < C; ++c) acc[c] *= fade;
+            }
+            float p[HV][4];
+#pragma unroll
+            for (int hf = 0; hf < HV; ++hf)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    p[hf][i] = __builtin_amdgcn_exp2f(z[hf][i] - m);
+                    l += p[hf][i];
+                }
+            if (!whole) {
+#pragma unroll
+                for (int e = 0; e < NV; ++e)
+                    if (r0 + (e >> 2) * 16 + (e & 3) >= n)
+#pragma unroll
+                        for (int w = 0; w < VW; ++w) x.v[e][w] = 0;
+            }
+            // ---- O^T += V^T P^T
+            if constexpr (BF16) {
+                // a weight as the sum of two bf16 numbers, 16 significant bits: one alone would cost 2^-9 of it
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    f32x2_t pv;
+                    pv[0] = p[w >> 1][2 * (w & 1)];
+                    pv[1] = p[w >> 1][2 * (w & 1) + 1];
+                    const bf16x2_t h2 = __builtin_convertvector(pv, bf16x2_t);
+                    hi[w] = __builtin_bit_cast(uint32_t, h2);
+                    pv[0] -= __uint_as_float(hi[w] << 16);
+                    pv[1] -= __uint_as_float(hi[w] & 0xFFFF0000u);
+                    lo[w] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pv, bf16x2_t));
+                }
+                const bf16x8_t ph = __builtin_bit_cast(bf16x8_t, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+                const bf16x8_t pl = __builtin_bit_cast(bf16x8_t, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    uint32_t vt[4];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w)
+                        vt[w] = __builtin_amdgcn_perm(x.v[2 * w + 1][c >> 1], x.v[2 * w][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
+                    const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(vt[0], vt[1], vt[2], vt[3]));
+                    acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph, acc[c], 0, 0, 0);
+                    acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl, acc[c], 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int c = 0; c < C; ++c)
+                        acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[i][c]), p[0][i], acc[c], 0, 0, 0);
+            }
+            if (t + 4 < tb) load_v(x, t + 4);
+        }
+
+        // ---- the four waves' parts, through LDS: lane (lq, lj) holds head dimensions 4 C lj .. 4 C (lj + 1) - 1 of query lq
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (lq < gt) {
+            if (lj == 0) {
+                red_m[wave][lq] = m;
+                red_l[wave][lq] = l;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < C; c += 4)
+                    *reinterpret_cast<f32x4_t *>(&red[wave][lq][(4 * lj + i) * C + c]) =
+                        f32x4_t{acc[c][i], acc[c + 1][i], acc[c + 2][i], acc[c + 3][i]};
         }
         __syncthreads();
-        part[tid] = acc;
-        __syncthreads();
-        if (tid < D) {
-            float sum = 0.0f;
-            for (int i = 0; i < 256 / D; ++i) sum += part[i * D + tid];
-            float *out = a.partial + (((long long)s * a.Hq + qh) * a.splits + sp) * (D + 2);
-            out[2 + tid] = sum;
-            if (tid == 0) {
-                out[0] = m;
-                out[1] = l;
+        const bool all = ta == 0 && tb == ts;            // nobody else has a part of this pair
+        const int slot = 2 * b + (t0 == run0 ? 0 : 1);
+        for (int i = tid; i < gt * D; i += 256) {
+            const int q = i / D, e = i % D;
+            float top = red_m[0][q];
+#pragma unroll
+            for (int w = 1; w < 4; ++w) top = fmaxf(top, red_m[w][q]);
+            float sum = 0.0f, lsum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float f = __builtin_amdgcn_exp2f(red_m[w][q] - top);
+                sum = fmaf(red[w][q][e], f, sum);
+                lsum = fmaf(red_l[w][q], f, lsum);
+            }
+            if (all) {
+                a.O[(qrow + q) * D + e] = sum / lsum;
+                if (e == 0) {
+                    const float z = top + __builtin_amdgcn_logf(lsum);
+                    a.stats[qrow + q] = z;
+                    if (a.lse != nullptr) a.lse[qrow + q] = z * 0.693147180559945309f;
+                }
+            } else {
+                const int gs = min(kPagedQueries, g);
+                a.slots[((long long)slot * gs + q) * D + e] = sum;
+                if (e == 0) {
+                    a.slot_stats[(slot * gs + q) * 2] = top;
+                    a.slot_stats[(slot * gs + q) * 2 + 1] = lsum;
+                }
             }
         }
+        if (ta == 0 && tid == 0) a.start[(long long)s * pairs + pair] = pair0;
         __syncthreads();
+        t0 = pair0 + tb;
     }
 }
 
-template <int D>
+template <bool BF16, int D>
 __global__ void __launch_bounds__(64)
-paged_join(AttendArgs a)
+paged_join(AttendArgs a, int groups)
 {
-    const long long row = blockIdx.x;
-    const float *p = a.partial + row * a.splits * (D + 2);
-    const int lane = threadIdx.x;
-    float m = -__builtin_inff();
-    for (int i = 0; i < a.splits; ++i) m = fmaxf(m, p[i * (D + 2)]);
-    float l = 0.0f, acc[D / 64] = {};
-    for (int i = 0; i < a.splits; ++i) {
-        const float *q = p + (long long)i * (D + 2);
-        if (q[1] == 0.0f) continue;                  // a split of no rows
-        const float f = exp2f(q[0] - m);
-        l += q[1] * f;
+    constexpr int TR = Shape<BF16, D>::TR;
+    const int row = blockIdx.x, lane = threadIdx.x;      // row: sequence and query head
+    const int g = a.Hq / a.H, s = row / a.Hq, qh = row % a.Hq, h = qh / g, q = qh % g;
+    const int n = paged_rows(a.len[s], a.per_seq << a.page_shift);
+    if (n == 0) {
 #pragma unroll
-        for (int e = 0; e < D / 64; ++e) acc[e] = fmaf(q[2 + e * 64 + lane], f, acc[e]);
+        for (int e = 0; e < D / 64; ++e) a.O[(long long)row * D + e * 64 + lane] = 0.0f;
+        if (lane == 0 && a.lse != nullptr) a.lse[row] = -__builtin_inff();
+        return;
+    }
+    const int total = *a.total, ts = (n + TR - 1) / TR;
+    const int pair0 = a.start[((long long)s * a.H + h) * a.tiles_q + q / kPagedQueries];
+    const int b0 = share_owner(total, groups, pair0), b1 = share_owner(total, groups, pair0 + ts - 1);
+    if (b0 == b1) return;                                // one workgroup had all of it and has written it
+    const int gs = min(kPagedQueries, g), ql = q % kPagedQueries;
+    const int slot0 = 2 * b0 + (share_start(total, groups, b0) == pair0 ? 0 : 1);
+    auto slot = [&](int b) { return (long long)(b == b0 ? slot0 : 2 * b) * gs + ql; };
+    float m = -__builtin_inff();
+    for (int b = b0 + lane; b <= b1; b += 64) m = fmaxf(m, a.slot_stats[slot(b) * 2]);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+    float l = 0.0f, acc[D / 64] = {};
+    for (int b = b0; b <= b1; ++b) {
+        const float f = __builtin_amdgcn_exp2f(a.slot_stats[slot(b) * 2] - m);
+        l = fmaf(a.slot_stats[slot(b) * 2 + 1], f, l);
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) acc[e] = fmaf(a.slots[slot(b) * D + e * 64 + lane], f, acc[e]);
     }
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) a.O[row * D + e * 64 + lane] = l > 0.0f ? acc[e] / l : 0.0f;
+    for (int e = 0; e < D / 64; ++e) a.O[(long long)row * D + e * 64 + lane] = acc[e] / l;
     if (lane == 0) {
-        const float all = l > 0.0f ? m + log2f(l) : -__builtin_inff();
-        a.stats[row] = all;
-        if (a.lse != nullptr) a.lse[row] = all * 0.693147180559945309f;
+        const float z = m + __builtin_amdgcn_logf(l);
+        a.stats[row] = z;
+        if (a.lse != nullptr) a.lse[row] = z * 0.693147180559945309f;
     }
 }
 
 __global__ void __launch_bounds__(256)
 paged_weights(AttendArgs a)
 {
-    const int cap = a.per_seq * a.page;
+    const int cap = a.per_seq << a.page_shift;
     const int pair = blockIdx.y + blockIdx.z * gridDim.y;
     if (pair >= a.S * a.H) return;
     const int s = pair / a.H, h = pair % a.H, g = a.Hq / a.H;
     const int r = blockIdx.x * 256 + threadIdx.x;
     if (r >= paged_rows(a.len[s], cap)) return;
     const long long at = (long long)pair * cap + r;
-    float w = a.mass_in != nullptr ? a.decay * a.mass_in[at] : 0.0f;
+    float w = 0.0f;
     for (int j = 0; j < g; ++j) {
         const long long q = (long long)s * a.Hq + h * g + j;
-        w += exp2f(a.logits[q * cap + r] - a.stats[q]);
+        w += __builtin_amdgcn_exp2f(a.logits[q * cap + r] - a.stats[q]);
     }
-    a.mass_out[at] = w;
+    a.mass_out[at] = a.mass_in != nullptr ? fmaf(a.decay, a.mass_in[at], w) : w;
 }
 
 }  // namespace
@@ -152,28 +413,37 @@ paged_weights(AttendArgs a)
 hipError_t launch_paged_attend(const ws_paged_cache &c, const void *Q, int Hq, float scale, float *O, float *lse, float decay,
                                const float *mass_in, float *mass_out, void *ws, hipStream_t st)
 {
+    const bool bf16 = c.dt == WS_BF16;
     const int cap = c.per_seq * c.page;
-    const PagedAttendSpace sp = paged_attend_space(c.S, c.Hkv, Hq, cap, c.d, mass_out != nullptr);
+    const PagedAttendSpace sp = paged_attend_space(bf16, c.S, c.Hkv, Hq, cap, c.d, mass_out != nullptr);
     AttendArgs a = {};
     a.K = c.K, a.V = c.V, a.Q = Q, a.table = c.table, a.len = c.len;
-    a.pages = c.pages, a.H = c.Hkv, a.page = c.page, a.S = c.S, a.per_seq = c.per_seq, a.Hq = Hq;
-    a.splits = paged_splits(c.S, c.Hkv, cap);
+    a.pages = c.pages, a.H = c.Hkv, a.page_shift = __builtin_ctz((unsigned)c.page), a.S = c.S, a.per_seq = c.per_seq, a.Hq = Hq;
+    a.tiles_q = paged_query_tiles(Hq / c.Hkv);
     a.scale_log2 = scale * 1.4426950408889634f;
     char *base = reinterpret_cast<char *>(ws);
-    a.partial = reinterpret_cast<float *>(base + sp.partial);
+    a.total = reinterpret_cast<int32_t *>(base);
+    a.start = reinterpret_cast<int32_t *>(base + sp.start);
     a.stats = reinterpret_cast<float *>(base + sp.stats);
+    a.slot_stats = reinterpret_cast<float *>(base + sp.slot_stats);
+    a.slots = reinterpret_cast<float *>(base + sp.slots);
     a.logits = mass_out ? reinterpret_cast<float *>(base + sp.logits) : nullptr;
     a.O = O, a.lse = lse, a.mass_in = mass_in, a.mass_out = mass_out, a.decay = decay;
-    const dim3 grid((unsigned)(c.S * c.Hkv * a.splits)), block(256);
-    if (c.dt == WS_BF16 && c.d == 64) hipLaunchKernelGGL((paged_split<true, 64>), grid, block, 0, st, a);
-    else if (c.dt == WS_BF16) hipLaunchKernelGGL((paged_split<true, 128>), grid, block, 0, st, a);
-    else if (c.d == 64) hipLaunchKernelGGL((paged_split<false, 64>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((paged_split<false, 128>), grid, block, 0, st, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (c.d == 64) hipLaunchKernelGGL((paged_join<64>), dim3((unsigned)(c.S * Hq)), dim3(64), 0, st, a);
-    else hipLaunchKernelGGL((paged_join<128>), dim3((unsigned)(c.S * Hq)), dim3(64), 0, st, a);
-    e = hipGetLastError();
+    const int groups = paged_groups(bf16, c.S, c.Hkv, Hq, cap);
+    auto go = [&](auto BF, auto DD) {
+        constexpr bool B = decltype(BF)::value;
+        constexpr int D = decltype(DD)::value;
+        const dim3 grid((unsigned)groups), block(256);
+        if (mass_out) hipLaunchKernelGGL((paged_split<B, D, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((paged_split<B, D, false>), grid, block, 0, st, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((paged_join<B, D>), dim3((unsigned)(c.S * Hq)), dim3(64), 0, st, a, groups);
+        return hipGetLastError();
+    };
+    using std::integral_constant;
+    const hipError_t e = bf16 ? (c.d == 64 ? go(std::true_type(), integral_constant<int, 64>()) : go(std::true_type(), integral_constant<int, 128>()))
+                              : (c.d == 64 ? go(std::false_type(), integral_constant<int, 64>()) : go(std::false_type(), integral_constant<int, 128>()));
     if (e != hipSuccess || !mass_out) return e;
     const int pairs = c.S * c.Hkv, y = pairs < 32768 ? pairs : 32768;
     hipLaunchKernelGGL(paged_weights, dim3((unsigned)((cap + 255) / 256), (unsigned)y, (unsigned)((pairs + y - 1) / y)), dim3(256), 0,

@@ -7,33 +7,43 @@ namespace ws {
 
 constexpr int kMaxAxes = 4;
 
-// Sizes for the attention's workspace: partial rows of the splits, statistics of every query head, and with weights the logits.
-constexpr int kPagedSplitTarget = 1024;     // workgroups a launch aims at
-constexpr int kPagedUnit = 128;             // rows of the smallest split
-
-static inline int paged_splits(int S, int Hkv, int cap)
+// How a launch of the attention is shared out.  The rows of all (sequence, KV head, up to 16 of its query heads) are counted off in
+// tiles, and every workgroup takes an equal run of tiles, across the borders of heads and sequences.
+constexpr int kPagedGroups = 768;           // workgroups of a full launch: three per compute unit
+constexpr int kPagedQueries = 16;           // query heads a workgroup serves from one reading of the rows: the matrix tile's width
+static inline int paged_tile_rows(bool bf16) { return bf16 ? 32 : 16; }
+static inline int paged_query_tiles(int g) { return (g + kPagedQueries - 1) / kPagedQueries; }
+// most tiles there can be (the lengths are on the device)
+static inline long long paged_most_tiles(bool bf16, int S, int Hkv, int Hq, int cap)
 {
-    const long long pairs = (long long)S * Hkv;
-    const long long want = (kPagedSplitTarget + pairs - 1) / pairs, most = (cap + kPagedUnit - 1) / kPagedUnit;
-    return (int)(want < most ? want : most);
+    const int tr = paged_tile_rows(bf16);
+    return (long long)S * Hkv * paged_query_tiles(Hq / Hkv) * ((cap + tr - 1) / tr);
+}
+static inline int paged_groups(bool bf16, int S, int Hkv, int Hq, int cap)
+{
+    const long long want = (paged_most_tiles(bf16, S, Hkv, Hq, cap) + 3) / 4;        // four waves, a tile each
+    return (int)(want < kPagedGroups ? want : kPagedGroups);
 }
 
 struct PagedAttendSpace {
-    size_t partial, stats, logits, bytes;   // offsets, total
+    size_t start, stats, slot_stats, slots, logits, bytes;   // offsets, total; the first 256 bytes hold the number of tiles
 };
-static inline PagedAttendSpace paged_attend_space(int S, int Hkv, int Hq, int cap, int d, bool weights)
+static inline PagedAttendSpace paged_attend_space(bool bf16, int S, int Hkv, int Hq, int cap, int d, bool weights)
 {
     PagedAttendSpace p;
-    const size_t rows = (size_t)S * Hq;
-    p.partial = 0;
-    p.stats = round_up(rows * paged_splits(S, Hkv, cap) * (d + 2) * sizeof(float), 256);
-    p.logits = p.stats + round_up(rows * sizeof(float), 256);
-    p.bytes = p.logits + (weights ? round_up(rows * cap * sizeof(float), 256) : 0);
+    const int g = Hq / Hkv, gt = g < kPagedQueries ? g : kPagedQueries;
+    const size_t slots = 2 * (size_t)paged_groups(bf16, S, Hkv, Hq, cap);
+    p.start = 256;
+    p.stats = p.start + round_up((size_t)S * Hkv * paged_query_tiles(g) * sizeof(int32_t), 256);
+    p.slot_stats = p.stats + round_up((size_t)S * Hq * sizeof(float), 256);
+    p.slots = p.slot_stats + round_up(slots * gt * 2 * sizeof(float), 256);
+    p.logits = p.slots + round_up(slots * gt * d * sizeof(float), 256);
+    p.bytes = p.logits + (weights ? round_up((size_t)S * Hq * cap * sizeof(float), 256) : 0);
     return p;
 }
-static inline size_t paged_attend_workspace_bytes(int S, int Hkv, int Hq, int cap, int d, bool weights)
+static inline size_t paged_attend_workspace_bytes(bool bf16, int S, int Hkv, int Hq, int cap, int d, bool weights)
 {
-    return paged_attend_space(S, Hkv, Hq, cap, d, weights).bytes;
+    return paged_attend_space(bf16, S, Hkv, Hq, cap, d, weights).bytes;
 }
 
 // Per KV head of a sequence: how many rows move, and from where to where.
