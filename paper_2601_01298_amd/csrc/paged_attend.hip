@@ -27,6 +27,18 @@ typedef __attribute__((ext_vector_type(2))) float f32x2_t;
 
 namespace {
 
+// What no kernel here writes and every lane of a wave reads alike is read through the scalar cache.
+typedef const __attribute__((address_space(4))) int32_t *scalar_i32;
+__device__ __forceinline__ scalar_i32 as_scalar(const int32_t *p) { return (scalar_i32)(uintptr_t)p; }
+
+// The cache's rows are read once: marked as such they leave the chip's caches to everything else.
+__device__ __forceinline__ uint4 load16(const void *p)
+{
+    typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+    const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p));
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
 struct AttendArgs {
     const void *K, *V, *Q;
     const int32_t *table, *len;
@@ -35,11 +47,12 @@ struct AttendArgs {
     int32_t *total, *start;                  // [1] tiles in all; [S,H,tiles_q] first tile of every pair
     float *stats;                            // [S,Hq] log2 of the sum of all weights
     float *slot_stats, *slots;               // [2 * groups][gt][2], [2 * groups][gt][D]
-    float *logits;                           // [S,Hq,cap] or NULL
+    float *logits;                           // [S,H][logit_rows(cap) / TR][g][TR] or NULL: a tile's logits of all query heads lie together
     float *O, *lse;
     const float *mass_in;
     float *mass_out;
     float decay;
+    int aligned;                             // the accounts can be read and written 16 bytes at a time
 };
 
 // An equal share of `total` tiles for each of `groups`: group b's run starts at ...
@@ -115,7 +128,7 @@ paged_split(AttendArgs a)
         s = l * each;
         first = (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l)) * pairs;
         for (;;) {
-            const int ts = (paged_rows(a.len[s], cap) + TR - 1) / TR * pairs;
+            const int ts = (paged_rows(as_scalar(a.len)[s], cap) + TR - 1) / TR * pairs;
             if (t0 < first + ts) break;
             first += ts;
             ++s;
@@ -123,7 +136,7 @@ paged_split(AttendArgs a)
     }
     const int run0 = t0;
     while (t0 < t1) {
-        const int n = paged_rows(a.len[s], cap);
+        const int n = paged_rows(as_scalar(a.len)[s], cap);
         const int ts = (n + TR - 1) / TR;                // tiles of a pair of this sequence
         if (ts == 0 || t0 >= first + ts * pairs) {
             first += ts * pairs;
@@ -136,7 +149,8 @@ paged_split(AttendArgs a)
         const int h = pair / a.tiles_q, q0 = pair % a.tiles_q * kPagedQueries;
         const int gt = min(kPagedQueries, g - q0);
         const long long qrow = (long long)s * a.Hq + h * g + q0;
-        const int32_t *table = a.table + (long long)s * a.per_seq;
+        float *logits = a.logits + (WEIGHTS ? ((long long)(s * a.H + h) * logit_rows(cap) * g + q0 * TR) : 0);
+        const scalar_i32 table = as_scalar(a.table) + (long long)s * a.per_seq;
         const int last16 = (n - 1) & ~15;                // a tile's second half may not exist: it reads this one instead
 
         // queries: the lane's part of query lq's row, in the order of the K loads; heads that do not exist are zero
@@ -147,34 +161,37 @@ paged_split(AttendArgs a)
             if (lq < gt)
                 qf[kk] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(a.Q) + (qrow + lq) * RB + kk * 64 + lj * 16);
         }
-        auto half_base = [&](int t, int hf) {            // where half hf of tile t starts in the pools
-            const int r = min(t * TR + 16 * hf, last16);
-            const int p = table[r >> a.page_shift];
-            return (unsigned long long)(paged_base(p, a.pages, a.H, h, 1 << a.page_shift) + (r & pmask)) * RB;
+        auto pages_of = [&](int t, int (&id)[HV]) {
+#pragma unroll
+            for (int hf = 0; hf < HV; ++hf) id[hf] = table[min(t * TR + 16 * hf, last16) >> a.page_shift];
         };
-        const int koff = lq * RB + lj * 16, voff = 4 * lj * RB + lq * VW * 4;
-        auto load_k = [&](Tile<BF16, D> &x, int t) {
+        auto half_base = [&](int t, int hf, int id) {    // where half hf of tile t starts in the pools
+            const int r = min(t * TR + 16 * hf, last16);
+            return (unsigned long long)(paged_base(id, a.pages, a.H, h, 1 << a.page_shift) + (r & pmask)) * RB;
+        };
+        const unsigned koff = lq * RB + lj * 16, voff = 4 * lj * RB + lq * VW * 4;
+        auto load_k = [&](Tile<BF16, D> &x, int t, const int (&id)[HV]) {
 #pragma unroll
             for (int hf = 0; hf < HV; ++hf) {
-                const char *p = reinterpret_cast<const char *>(a.K) + half_base(t, hf);
+                const char *p = reinterpret_cast<const char *>(a.K) + half_base(t, hf, id[hf]);
 #pragma unroll
-                for (int kk = 0; kk < NK; ++kk) x.k[hf][kk] = *reinterpret_cast<const uint4 *>(p + koff + kk * 64);
+                for (int kk = 0; kk < NK; ++kk) x.k[hf][kk] = load16(p + koff + kk * 64);
             }
         };
-        auto load_v = [&](Tile<BF16, D> &x, int t) {
+        auto load_v = [&](Tile<BF16, D> &x, int t, const int (&id)[HV]) {
 #pragma unroll
             for (int hf = 0; hf < HV; ++hf) {
-                const char *p = reinterpret_cast<const char *>(a.V) + half_base(t, hf);
+                const char *p = reinterpret_cast<const char *>(a.V) + half_base(t, hf, id[hf]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t *src = reinterpret_cast<const uint32_t *>(p + voff + i * RB);
                     if constexpr (VW == 2) {
-                        const uint2 w = *reinterpret_cast<const uint2 *>(src);
-                        x.v[4 * hf + i][0] = w.x, x.v[4 * hf + i][1] = w.y;
+                        typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+                        const u32x2_t w = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t *>(p + voff + i * RB));
+                        x.v[4 * hf + i][0] = w[0], x.v[4 * hf + i][1] = w[1];
                     } else {
 #pragma unroll
                         for (int j = 0; j < VW / 4; ++j) {
-                            const uint4 w = *reinterpret_cast<const uint4 *>(src + 4 * j);
+                            const uint4 w = load16(p + voff + i * RB + 16 * j);
                             x.v[4 * hf + i][4 * j] = w.x, x.v[4 * hf + i][4 * j + 1] = w.y;
                             x.v[4 * hf + i][4 * j + 2] = w.z, x.v[4 * hf + i][4 * j + 3] = w.w;
                         }
@@ -189,13 +206,14 @@ paged_split(AttendArgs a)
         for (int c = 0; c < C; ++c) acc[c] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
         Tile<BF16, D> x;
-        int t = ta + wave;
-        if (t < tb) {
-            load_k(x, t);
-            load_v(x, t);
-        }
-        for (; t < tb; t += 4) {
-            // ---- scores of rows 16 hf + 4 lj + i for query lq
+        int id[HV];                                      // pages of the tile to load next
+        // One tile, held in x.  MORE: the wave's next tile, t + 4, is loaded behind the last use of K and of V (so one of the two
+        // is always on its way), and the pages of the one after it are looked up; a tile with another one behind it is whole.
+        auto tile = [&](int t, auto more) {
+            constexpr bool MORE = decltype(more)::value;
+            int id2[HV];
+            if constexpr (MORE) pages_of(t + 8, id2);
+            // scores of rows 16 hf + 4 lj + i for query lq
             f32x4_t z[HV];
 #pragma unroll
             for (int hf = 0; hf < HV; ++hf) {
@@ -214,9 +232,8 @@ paged_split(AttendArgs a)
                     }
                 }
             }
-            if (t + 4 < tb) load_k(x, t + 4);
+            if constexpr (MORE) load_k(x, t + 4, id);
             const int r0 = t * TR + 4 * lj;              // the lane's first row
-            const bool whole = (t + 1) * TR <= n;
             float top = -__builtin_inff();
 #pragma unroll
             for (int hf = 0; hf < HV; ++hf)
@@ -224,14 +241,14 @@ paged_split(AttendArgs a)
                 for (int i = 0; i < 4; ++i) {
                     z[hf][i] *= a.scale_log2;
                     // rows behind the sequence's last one hold anything: their score is replaced, and so is their V below
-                    if (!whole && r0 + 16 * hf + i >= n) z[hf][i] = -__builtin_inff();
+                    if (!MORE && r0 + 16 * hf + i >= n) z[hf][i] = -__builtin_inff();
                     top = fmaxf(top, z[hf][i]);
                 }
             if (WEIGHTS && lq < gt) {
-                float *to = a.logits + (qrow + lq) * cap + r0;
+                float *to = logits + ((long long)t * g + lq) * TR + 4 * lj;
 #pragma unroll
                 for (int hf = 0; hf < HV; ++hf)
-                    if (whole || r0 + 16 * hf < n) *reinterpret_cast<f32x4_t *>(to + 16 * hf) = z[hf];
+                    if (MORE || r0 + 16 * hf < n) *reinterpret_cast<f32x4_t *>(to + 16 * hf) = z[hf];
             }
             // the reference is moved only when a score exceeds it by more than 2^8: weights stay far from overflow, and the
             // accumulator is rescaled a few times per pass instead of once per tile.  (All four lanes of a query agree.)
@@ -253,30 +270,30 @@ paged_split(AttendArgs a)
                     p[hf][i] = __builtin_amdgcn_exp2f(z[hf][i] - m);
                     l += p[hf][i];
                 }
-            if (!whole) {
+            if constexpr (!MORE) {
 #pragma unroll
                 for (int e = 0; e < NV; ++e)
-                    if (r0 + (e >> 2) * 16 + (e & 3) >= n)
 #pragma unroll
-                        for (int w = 0; w < VW; ++w) x.v[e][w] = 0;
+                    for (int w = 0; w < VW; ++w) x.v[e][w] = r0 + (e >> 2) * 16 + (e & 3) >= n ? 0u : x.v[e][w];
             }
-            // ---- O^T += V^T P^T
+            // O^T += V^T P^T
             if constexpr (BF16) {
-                // a weight as the sum of two bf16 numbers, 16 significant bits: one alone would cost 2^-9 of it
-                uint32_t hi[4], lo[4];
+                // a weight as the sum of three bf16 numbers, all its 24 bits: one alone would cost 2^-9 of it, two 2^-17, which
+                // shows in the output (the matrix cores have the time)
+                uint32_t part[3][4];
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     f32x2_t pv;
                     pv[0] = p[w >> 1][2 * (w & 1)];
                     pv[1] = p[w >> 1][2 * (w & 1) + 1];
-                    const bf16x2_t h2 = __builtin_convertvector(pv, bf16x2_t);
-                    hi[w] = __builtin_bit_cast(uint32_t, h2);
-                    pv[0] -= __uint_as_float(hi[w] << 16);
-                    pv[1] -= __uint_as_float(hi[w] & 0xFFFF0000u);
-                    lo[w] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pv, bf16x2_t));
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) {
+                        const uint32_t two = __builtin_bit_cast(uint32_t, __builtin_convertvector(pv, bf16x2_t));
+                        part[k][w] = two;
+                        pv[0] -= __uint_as_float(two << 16);
+                        pv[1] -= __uint_as_float(two & 0xFFFF0000u);
+                    }
                 }
-                const bf16x8_t ph = __builtin_bit_cast(bf16x8_t, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-                const bf16x8_t pl = __builtin_bit_cast(bf16x8_t, make_uint4(lo[0], lo[1], lo[2], lo[3]));
 #pragma unroll
                 for (int c = 0; c < C; ++c) {
                     uint32_t vt[4];
@@ -284,8 +301,10 @@ paged_split(AttendArgs a)
                     for (int w = 0; w < 4; ++w)
                         vt[w] = __builtin_amdgcn_perm(x.v[2 * w + 1][c >> 1], x.v[2 * w][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
                     const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(vt[0], vt[1], vt[2], vt[3]));
-                    acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph, acc[c], 0, 0, 0);
-                    acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl, acc[c], 0, 0, 0);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k)
+                        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            vf, __builtin_bit_cast(bf16x8_t, make_uint4(part[k][0], part[k][1], part[k][2], part[k][3])), acc[c], 0, 0, 0);
                 }
             } else {
 #pragma unroll
@@ -294,7 +313,20 @@ paged_split(AttendArgs a)
                     for (int c = 0; c < C; ++c)
                         acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[i][c]), p[0][i], acc[c], 0, 0, 0);
             }
-            if (t + 4 < tb) load_v(x, t + 4);
+            if constexpr (MORE) {
+                load_v(x, t + 4, id);
+#pragma unroll
+                for (int hf = 0; hf < HV; ++hf) id[hf] = id2[hf];
+            }
+        };
+        int t = ta + wave;
+        if (t < tb) {
+            pages_of(t, id);
+            load_k(x, t, id);
+            load_v(x, t, id);
+            pages_of(t + 4, id);
+            for (; t + 4 < tb; t += 4) tile(t, std::true_type());
+            tile(t, std::false_type());
         }
 
         // ---- the four waves' parts, through LDS: lane (lq, lj) holds head dimensions 4 C lj .. 4 C (lj + 1) - 1 of query lq
@@ -349,63 +381,141 @@ paged_split(AttendArgs a)
     }
 }
 
+// What several workgroups left of one query head: their statistics, and where their parts lie.
+struct Parts {
+    int b0, b1, slot0, gs, ql;
+    __device__ long long slot(int b) const { return (long long)(b == b0 ? slot0 : 2 * b) * gs + ql; }
+};
+template <int TR>
+__device__ __forceinline__ Parts parts_of(const AttendArgs &a, int groups, int s, int h, int q, int n)
+{
+    Parts p;
+    const int total = *a.total, ts = (n + TR - 1) / TR;
+    const int pair0 = a.start[((long long)s * a.H + h) * a.tiles_q + q / kPagedQueries];
+    p.b0 = share_owner(total, groups, pair0);
+    p.b1 = share_owner(total, groups, pair0 + ts - 1);
+    p.slot0 = 2 * p.b0 + (share_start(total, groups, p.b0) == pair0 ? 0 : 1);
+    p.gs = min(kPagedQueries, a.Hq / a.H);
+    p.ql = q % kPagedQueries;
+    return p;
+}
+
+// One workgroup per query head of a sequence: its parts, if it has several, to their common maximum.
 template <bool BF16, int D>
-__global__ void __launch_bounds__(64)
-paged_join(AttendArgs a, int groups)
+__device__ void join_row(const AttendArgs &a, int groups, int row)
 {
     constexpr int TR = Shape<BF16, D>::TR;
-    const int row = blockIdx.x, lane = threadIdx.x;      // row: sequence and query head
+    __shared__ float factor[kPagedGroups];
+    __shared__ float red[4][D], red_l[4], red_m[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int g = a.Hq / a.H, s = row / a.Hq, qh = row % a.Hq, h = qh / g, q = qh % g;
     const int n = paged_rows(a.len[s], a.per_seq << a.page_shift);
     if (n == 0) {
-#pragma unroll
-        for (int e = 0; e < D / 64; ++e) a.O[(long long)row * D + e * 64 + lane] = 0.0f;
-        if (lane == 0 && a.lse != nullptr) a.lse[row] = -__builtin_inff();
+        if (tid < D) a.O[(long long)row * D + tid] = 0.0f;
+        if (tid == 0 && a.lse != nullptr) a.lse[row] = -__builtin_inff();
         return;
     }
-    const int total = *a.total, ts = (n + TR - 1) / TR;
-    const int pair0 = a.start[((long long)s * a.H + h) * a.tiles_q + q / kPagedQueries];
-    const int b0 = share_owner(total, groups, pair0), b1 = share_owner(total, groups, pair0 + ts - 1);
-    if (b0 == b1) return;                                // one workgroup had all of it and has written it
-    const int gs = min(kPagedQueries, g), ql = q % kPagedQueries;
-    const int slot0 = 2 * b0 + (share_start(total, groups, b0) == pair0 ? 0 : 1);
-    auto slot = [&](int b) { return (long long)(b == b0 ? slot0 : 2 * b) * gs + ql; };
+    const Parts p = parts_of<TR>(a, groups, s, h, q, n);
+    if (p.b0 == p.b1) return;                            // one workgroup had all of it and has written it
     float m = -__builtin_inff();
-    for (int b = b0 + lane; b <= b1; b += 64) m = fmaxf(m, a.slot_stats[slot(b) * 2]);
+    for (int b = p.b0 + tid; b <= p.b1; b += 256) m = fmaxf(m, a.slot_stats[p.slot(b) * 2]);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-    float l = 0.0f, acc[D / 64] = {};
-    for (int b = b0; b <= b1; ++b) {
-        const float f = __builtin_amdgcn_exp2f(a.slot_stats[slot(b) * 2] - m);
-        l = fmaf(a.slot_stats[slot(b) * 2 + 1], f, l);
+    if (lane == 0) red_m[wave] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
+    float l = 0.0f;
+    for (int b = p.b0 + tid; b <= p.b1; b += 256) {
+        const float f = __builtin_amdgcn_exp2f(a.slot_stats[p.slot(b) * 2] - m);
+        factor[b - p.b0] = f;
+        l = fmaf(a.slot_stats[p.slot(b) * 2 + 1], f, l);
+    }
+    l = lane_group_sum<64>(l);
+    if (lane == 0) red_l[wave] = l;
+    __syncthreads();
+    l = red_l[0] + red_l[1] + red_l[2] + red_l[3];
+    float acc[D / 64] = {};
+#pragma unroll 4
+    for (int b = p.b0 + wave; b <= p.b1; b += 4) {
+        const float f = factor[b - p.b0];
 #pragma unroll
-        for (int e = 0; e < D / 64; ++e) acc[e] = fmaf(a.slots[slot(b) * D + e * 64 + lane], f, acc[e]);
+        for (int e = 0; e < D / 64; ++e) acc[e] = fmaf(a.slots[p.slot(b) * D + e * 64 + lane], f, acc[e]);
     }
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) a.O[(long long)row * D + e * 64 + lane] = acc[e] / l;
-    if (lane == 0) {
-        const float z = m + __builtin_amdgcn_logf(l);
-        a.stats[row] = z;
-        if (a.lse != nullptr) a.lse[row] = z * 0.693147180559945309f;
+    for (int e = 0; e < D / 64; ++e) red[wave][e * 64 + lane] = acc[e];
+    __syncthreads();
+    if (tid < D) a.O[(long long)row * D + tid] = (red[0][tid] + red[1][tid] + red[2][tid] + red[3][tid]) / l;
+    if (tid == 0 && a.lse != nullptr) a.lse[row] = (m + __builtin_amdgcn_logf(l)) * 0.693147180559945309f;
+}
+
+// One workgroup per 1024 rows of a (sequence, KV head): what the rows received is added to their accounts.
+template <bool BF16, int D>
+__device__ void add_weights(const AttendArgs &a, int groups, int pair, int chunk)
+{
+    constexpr int TR = Shape<BF16, D>::TR;
+    __shared__ float stat[256];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int cap = a.per_seq << a.page_shift;
+    const int s = pair / a.H, h = pair % a.H, g = a.Hq / a.H;
+    const int n = paged_rows(a.len[s], cap);
+    if (chunk * 1024 >= n) return;
+    const int r = chunk * 1024 + tid * 4;
+    const float *z = a.logits + ((long long)pair * logit_rows(cap) + r / TR * TR) * g + r % TR;
+    float w[4] = {};
+    for (int q0 = 0; q0 < g; q0 += 256) {
+        if (q0 > 0) __syncthreads();
+        // the sum of all weights of query head q, log2: as written by the one workgroup that had it all, or from its parts
+        for (int q = q0 + wave; q < min(g, q0 + 256); q += 4) {
+            const Parts p = parts_of<TR>(a, groups, s, h, q, n);
+            float all;
+            if (p.b0 == p.b1) {
+                all = a.stats[(long long)s * a.Hq + h * g + q];
+            } else {
+                float m = -__builtin_inff(), l = 0.0f;
+                for (int b = p.b0 + lane; b <= p.b1; b += 64) m = fmaxf(m, a.slot_stats[p.slot(b) * 2]);
+#pragma unroll
+                for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+                for (int b = p.b0 + lane; b <= p.b1; b += 64)
+                    l = fmaf(a.slot_stats[p.slot(b) * 2 + 1], __builtin_amdgcn_exp2f(a.slot_stats[p.slot(b) * 2] - m), l);
+                all = m + __builtin_amdgcn_logf(lane_group_sum<64>(l));
+            }
+            if (lane == 0) stat[q - q0] = all;
+        }
+        __syncthreads();
+        if (r < n)
+#pragma unroll 4
+            for (int q = q0; q < min(g, q0 + 256); ++q) {
+                const f32x4_t x = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t *>(z + (long long)q * TR));
+                const float all = stat[q - q0];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] += __builtin_amdgcn_exp2f(x[i] - all);
+            }
+    }
+    if (r >= n) return;
+    const long long at = (long long)pair * cap + r;
+    if (r + 4 <= n && a.aligned) {
+        f32x4_t x = {w[0], w[1], w[2], w[3]};
+        if (a.mass_in != nullptr) {
+            const f32x4_t old = *reinterpret_cast<const f32x4_t *>(a.mass_in + at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = fmaf(a.decay, old[i], w[i]);
+        }
+        *reinterpret_cast<f32x4_t *>(a.mass_out + at) = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (r + i < n) a.mass_out[at + i] = a.mass_in != nullptr ? fmaf(a.decay, a.mass_in[at + i], w[i]) : w[i];
     }
 }
 
+template <bool BF16, int D>
 __global__ void __launch_bounds__(256)
-paged_weights(AttendArgs a)
+paged_finish(AttendArgs a, int groups, int chunks)
 {
-    const int cap = a.per_seq << a.page_shift;
-    const int pair = blockIdx.y + blockIdx.z * gridDim.y;
-    if (pair >= a.S * a.H) return;
-    const int s = pair / a.H, h = pair % a.H, g = a.Hq / a.H;
-    const int r = blockIdx.x * 256 + threadIdx.x;
-    if (r >= paged_rows(a.len[s], cap)) return;
-    const long long at = (long long)pair * cap + r;
-    float w = 0.0f;
-    for (int j = 0; j < g; ++j) {
-        const long long q = (long long)s * a.Hq + h * g + j;
-        w += __builtin_amdgcn_exp2f(a.logits[q * cap + r] - a.stats[q]);
-    }
-    a.mass_out[at] = a.mass_in != nullptr ? fmaf(a.decay, a.mass_in[at], w) : w;
+    const long long b = blockIdx.x + (long long)blockIdx.y * gridDim.x;
+    const int rows = a.S * a.Hq;
+    if (b < rows) join_row<BF16, D>(a, groups, (int)b);
+    else if (b - rows < (long long)a.S * a.H * chunks) add_weights<BF16, D>(a, groups, (int)((b - rows) / chunks), (int)((b - rows) % chunks));
 }
 
 }  // namespace
@@ -429,6 +539,7 @@ hipError_t launch_paged_attend(const ws_paged_cache &c, const void *Q, int Hq, f
     a.slots = reinterpret_cast<float *>(base + sp.slots);
     a.logits = mass_out ? reinterpret_cast<float *>(base + sp.logits) : nullptr;
     a.O = O, a.lse = lse, a.mass_in = mass_in, a.mass_out = mass_out, a.decay = decay;
+    a.aligned = ((reinterpret_cast<uintptr_t>(mass_in) | reinterpret_cast<uintptr_t>(mass_out)) & 15) == 0;
     const int groups = paged_groups(bf16, c.S, c.Hkv, Hq, cap);
     auto go = [&](auto BF, auto DD) {
         constexpr bool B = decltype(BF)::value;
@@ -438,17 +549,15 @@ hipError_t launch_paged_attend(const ws_paged_cache &c, const void *Q, int Hq, f
         else hipLaunchKernelGGL((paged_split<B, D, false>), grid, block, 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((paged_join<B, D>), dim3((unsigned)(c.S * Hq)), dim3(64), 0, st, a, groups);
+        const int chunks = mass_out ? (cap + 1023) / 1024 : 0;
+        const long long blocks = (long long)c.S * Hq + (long long)c.S * c.Hkv * chunks;
+        const unsigned x = blocks < (1 << 22) ? (unsigned)blocks : 1u << 22;
+        hipLaunchKernelGGL((paged_finish<B, D>), dim3(x, (unsigned)((blocks + x - 1) / x)), block, 0, st, a, groups, chunks);
         return hipGetLastError();
     };
     using std::integral_constant;
-    const hipError_t e = bf16 ? (c.d == 64 ? go(std::true_type(), integral_constant<int, 64>()) : go(std::true_type(), integral_constant<int, 128>()))
-                              : (c.d == 64 ? go(std::false_type(), integral_constant<int, 64>()) : go(std::false_type(), integral_constant<int, 128>()));
-    if (e != hipSuccess || !mass_out) return e;
-    const int pairs = c.S * c.Hkv, y = pairs < 32768 ? pairs : 32768;
-    hipLaunchKernelGGL(paged_weights, dim3((unsigned)((cap + 255) / 256), (unsigned)y, (unsigned)((pairs + y - 1) / y)), dim3(256), 0,
-                       st, a);
-    return hipGetLastError();
+    if (bf16) return c.d == 64 ? go(std::true_type(), integral_constant<int, 64>()) : go(std::true_type(), integral_constant<int, 128>());
+    return c.d == 64 ? go(std::false_type(), integral_constant<int, 64>()) : go(std::false_type(), integral_constant<int, 128>());
 }
 
 }  // namespace ws

@@ -25,6 +25,9 @@ static inline int paged_groups(bool bf16, int S, int Hkv, int Hq, int cap)
     return (int)(want < kPagedGroups ? want : kPagedGroups);
 }
 
+// whole tiles of logits per query head
+__host__ __device__ static inline int logit_rows(int cap) { return (cap + 31) / 32 * 32; }
+
 struct PagedAttendSpace {
     size_t start, stats, slot_stats, slots, logits, bytes;   // offsets, total; the first 256 bytes hold the number of tiles
 };
@@ -38,7 +41,7 @@ static inline PagedAttendSpace paged_attend_space(bool bf16, int S, int Hkv, int
     p.slot_stats = p.stats + round_up((size_t)S * Hq * sizeof(float), 256);
     p.slots = p.slot_stats + round_up(slots * gt * 2 * sizeof(float), 256);
     p.logits = p.slots + round_up(slots * gt * d * sizeof(float), 256);
-    p.bytes = p.logits + (weights ? round_up((size_t)S * Hq * cap * sizeof(float), 256) : 0);
+    p.bytes = p.logits + (weights ? round_up((size_t)S * Hq * logit_rows(cap) * sizeof(float), 256) : 0);
     return p;
 }
 static inline size_t paged_attend_workspace_bytes(bool bf16, int S, int Hkv, int Hq, int cap, int d, bool weights)
