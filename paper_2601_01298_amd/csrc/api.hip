@@ -62,7 +62,7 @@ size_t ws_synapse_workspace_bytes(ws_op op, ws_dtype dt, int H, int L, int d, in
     case WS_OP_PAGED_ATTEND:
         // H = KV heads, Hq = query heads, L = rows a sequence has room for, N = sequences, k != 0: with the rows' weights
         if (H < 1 || Hq < 1 || N < 1 || L < 1 || L >= kMaxL || Hq % H != 0 || (long long)N * Hq > (1 << 20) ||
-            ws::paged_most_tiles(dt == WS_BF16, N, H, Hq, L) > 0x7FFFFFFFLL)
+            ws::paged_most_tiles(dt == WS_BF16, N, H, Hq, L) > 0x7FFFFFFFLL || (k != 0 && !ws::paged_logits_fit(Hq / H, L)))
             return (size_t)-1;
         return ws::paged_attend_workspace_bytes(dt == WS_BF16, N, H, Hq, L, d, k != 0);
     case WS_OP_PAGED_EVICT:

@@ -87,6 +87,7 @@ ws_status ws_synapse_paged_attend(const ws_paged_cache *cache, const void *Q, in
     const int cap = cache->per_seq * cache->page;
     const bool bf16 = cache->dt == WS_BF16;
     if (ws::paged_most_tiles(bf16, cache->S, cache->Hkv, Hq, cap) > 0x7FFFFFFFLL) return WS_ERR_UNSUPPORTED;
+    if (mass_out && !ws::paged_logits_fit(Hq / cache->Hkv, cap)) return WS_ERR_UNSUPPORTED;
     s = check_ws(workspace, workspace_bytes, ws::paged_attend_workspace_bytes(bf16, cache->S, cache->Hkv, Hq, cap, cache->d, mass_out != nullptr));
     if (s != WS_OK) return s;
     if (scale <= 0.0f) scale = 1.0f / std::sqrt((float)cache->d);

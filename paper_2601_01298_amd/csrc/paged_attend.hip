@@ -24,6 +24,7 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
 namespace {
 
@@ -34,7 +35,6 @@ __device__ __forceinline__ scalar_i32 as_scalar(const int32_t *p) { return (scal
 // The cache's rows are read once: marked as such they leave the chip's caches to everything else.
 __device__ __forceinline__ uint4 load16(const void *p)
 {
-    typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
     const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p));
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
@@ -47,7 +47,7 @@ struct AttendArgs {
     int32_t *total, *start;                  // [1] tiles in all; [S,H,tiles_q] first tile of every pair
     float *stats;                            // [S,Hq] log2 of the sum of all weights
     float *slot_stats, *slots;               // [2 * groups][gt][2], [2 * groups][gt][D]
-    float *logits;                           // [S,H][logit_rows(cap) / TR][g][TR] or NULL: a tile's logits of all query heads lie together
+    float *logits;                           // [S,H][logit_rows(cap) / 16][g][16] or NULL: what a wave stores at once lies together
     float *O, *lse;
     const float *mass_in;
     float *mass_out;
@@ -85,19 +85,261 @@ struct Tile {
     uint32_t v[Shape<BF16, D>::NV][Shape<BF16, D>::VW];
 };
 
+constexpr int kNowhere = 0, kToMemory = 1, kToLds = 2;       // where the logits go, for the rows' weights
+
+// Room for the four waves' parts of a result; a row's length shifts the banks from query to query.
+template <int D>
+struct Merge {
+    float part[4][kPagedQueries][D + 4];
+    float m[4][kPagedQueries], l[4][kPagedQueries];
+    // the four parts of query q brought to their maximum: that, their sum of weights, and element e
+    __device__ __forceinline__ void query(int q, int e, float &top, float &lsum, float &sum) const
+    {
+        top = fmaxf(fmaxf(m[0][q], m[1][q]), fmaxf(m[2][q], m[3][q]));
+        sum = lsum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = __builtin_amdgcn_exp2f(m[w][q] - top);
+            sum = fmaf(part[w][q][e], f, sum);
+            lsum = fmaf(l[w][q], f, lsum);
+        }
+    }
+};
+
+// Tiles [ta, tb) of sequence s's head h (n rows) for query heads q0 .. of it; the waves' parts are left in `red`, behind a barrier.
+template <bool BF16, int D, int SINK>
+__device__ __forceinline__ void sweep(const AttendArgs &a, int s, int h, int q0, int n, int ta, int tb, Merge<D> &red, float *kept,
+                                      int kept_stride)
+{
+    using P = Shape<BF16, D>;
+    constexpr int TR = P::TR, RB = P::RB, HV = P::HV, NK = P::NK, C = P::C, VW = P::VW, NV = P::NV;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lq = lane & 15, lj = lane >> 4;
+    const int cap = a.per_seq << a.page_shift, pmask = (1 << a.page_shift) - 1;
+    const int g = a.Hq / a.H, gt = min(kPagedQueries, g - q0);
+    const long long qrow = (long long)s * a.Hq + h * g + q0;
+    __amdgpu_buffer_rsrc_t logits;
+    if constexpr (SINK == kToMemory) {
+        // the logits of this head's query heads, from the first one of this tile of them on
+        float *p = a.logits + ((long long)(s * a.H + h) * logit_rows(cap) * g + q0 * 16);
+        logits = __builtin_amdgcn_make_buffer_rsrc(p, 0, (logit_rows(cap) * g - q0 * 16) * 4, 0x00020000);
+    }
+    const scalar_i32 table = as_scalar(a.table) + (long long)s * a.per_seq;
+    const int last16 = (n - 1) & ~15;                // a tile's second half may not exist: it reads this one instead
+
+    // queries: the lane's part of query lq's row, in the order of the K loads; heads that do not exist are zero
+    uint4 qf[NK];
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) {
+        qf[kk] = make_uint4(0, 0, 0, 0);
+        if (lq < gt)
+            qf[kk] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(a.Q) + (qrow + lq) * RB + kk * 64 + lj * 16);
+    }
+    auto pages_of = [&](int t, int (&id)[HV]) {
+#pragma unroll
+        for (int hf = 0; hf < HV; ++hf) id[hf] = table[min(t * TR + 16 * hf, last16) >> a.page_shift];
+    };
+    auto half_base = [&](int t, int hf, int id) {    // where half hf of tile t starts in the pools
+        const int r = min(t * TR + 16 * hf, last16);
+        return (unsigned long long)(paged_base(id, a.pages, a.H, h, 1 << a.page_shift) + (r & pmask)) * RB;
+    };
+    const unsigned koff = lq * RB + lj * 16, voff = 4 * lj * RB + lq * VW * 4;
+    auto load_k = [&](Tile<BF16, D> &x, int t, const int (&id)[HV]) {
+#pragma unroll
+        for (int hf = 0; hf < HV; ++hf) {
+            const char *p = reinterpret_cast<const char *>(a.K) + half_base(t, hf, id[hf]);
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) x.k[hf][kk] = load16(p + koff + kk * 64);
+        }
+    };
+    auto load_v = [&](Tile<BF16, D> &x, int t, const int (&id)[HV]) {
+#pragma unroll
+        for (int hf = 0; hf < HV; ++hf) {
+            const char *p = reinterpret_cast<const char *>(a.V) + half_base(t, hf, id[hf]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (VW == 2) {
+                    typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+                    const u32x2_t w = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t *>(p + voff + i * RB));
+                    x.v[4 * hf + i][0] = w[0], x.v[4 * hf + i][1] = w[1];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < VW / 4; ++j) {
+                        const uint4 w = load16(p + voff + i * RB + 16 * j);
+                        x.v[4 * hf + i][4 * j] = w.x, x.v[4 * hf + i][4 * j + 1] = w.y;
+                        x.v[4 * hf + i][4 * j + 2] = w.z, x.v[4 * hf + i][4 * j + 3] = w.w;
+                    }
+                }
+            }
+        }
+    };
+
+    float m = -__builtin_inff(), l = 0.0f;           // of query lq; l of the lane's rows only
+    f32x4_t acc[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) acc[c] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+
+    Tile<BF16, D> x;
+    int id[HV];                                      // pages of the tile to load next
+    // One tile, held in x.  MORE: the wave's next tile, t + 4, is loaded behind the last use of K and of V (so one of the two
+    // is always on its way), and the pages of the one after it are looked up; a tile with another one behind it is whole.
+    auto tile = [&](int t, auto more) {
+        constexpr bool MORE = decltype(more)::value;
+        int id2[HV];
+        if constexpr (MORE) pages_of(t + 8, id2);
+        // scores of rows 16 hf + 4 lj + i for query lq
+        f32x4_t z[HV];
+#pragma unroll
+        for (int hf = 0; hf < HV; ++hf) {
+            z[hf] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) {
+                if constexpr (BF16) {
+                    z[hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x.k[hf][kk]),
+                                                                   __builtin_bit_cast(bf16x8_t, qf[kk]), z[hf], 0, 0, 0);
+                } else {
+                    const uint32_t kw[4] = {x.k[hf][kk].x, x.k[hf][kk].y, x.k[hf][kk].z, x.k[hf][kk].w};
+                    const uint32_t qw[4] = {qf[kk].x, qf[kk].y, qf[kk].z, qf[kk].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        z[hf] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kw[e]), __uint_as_float(qw[e]), z[hf], 0, 0, 0);
+                }
+            }
+        }
+        if constexpr (MORE) load_k(x, t + 4, id);
+        const int r0 = t * TR + 4 * lj;              // the lane's first row
+        float top = -__builtin_inff();
+#pragma unroll
+        for (int hf = 0; hf < HV; ++hf)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                z[hf][i] *= a.scale_log2;
+                // rows behind the sequence's last one hold anything: their score is replaced, and so is their V below
+                if (!MORE && r0 + 16 * hf + i >= n) z[hf][i] = -__builtin_inff();
+                top = fmaxf(top, z[hf][i]);
+            }
+        if constexpr (SINK == kToMemory) {
+            // Lanes of heads that do not exist store out of the buffer's range, which the hardware drops: behind a branch the
+            // compiler could not count these stores, and every tile would wait for the K it has just asked for.
+            const unsigned to = (unsigned)((t * HV * g + lq) * 16 + 4 * lj) * 4u;
+#pragma unroll
+            for (int hf = 0; hf < HV; ++hf) {
+                const bool there = lq < gt && (MORE || r0 + 16 * hf < n);
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, z[hf]), logits, there ? to + 64u * g * hf : 0xFFFFFFF0u, 0, 0);
+            }
+        }
+        if constexpr (SINK == kToLds) {
+            if (lq < gt)
+#pragma unroll
+                for (int hf = 0; hf < HV; ++hf)
+                    if (MORE || r0 + 16 * hf < n) *reinterpret_cast<f32x4_t *>(kept + lq * kept_stride + r0 + 16 * hf) = z[hf];
+        }
+        // the reference is moved only when a score exceeds it by more than 2^8: weights stay far from overflow, and the
+        // accumulator is rescaled a few times per pass instead of once per tile.  (All four lanes of a query agree.)
+        if (__any(top > m + 8.0f)) {
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float to = fmaxf(m, top);
+            const float fade = __builtin_amdgcn_exp2f(m - to);
+            m = to;
+            l *= fade;
+#pragma unroll
+            for (int c = 0; c < C; ++c) acc[c] *= fade;
+        }
+        float p[HV][4];
+#pragma unroll
+        for (int hf = 0; hf < HV; ++hf)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p[hf][i] = __builtin_amdgcn_exp2f(z[hf][i] - m);
+                l += p[hf][i];
+            }
+        if constexpr (!MORE) {
+#pragma unroll
+            for (int e = 0; e < NV; ++e)
+#pragma unroll
+                for (int w = 0; w < VW; ++w) x.v[e][w] = r0 + (e >> 2) * 16 + (e & 3) >= n ? 0u : x.v[e][w];
+        }
+        // O^T += V^T P^T
+        if constexpr (BF16) {
+            // a weight as the sum of three bf16 numbers, all its 24 bits: one alone would cost 2^-9 of it, two 2^-17, which
+            // shows in the output (the matrix cores have the time)
+            uint32_t part[3][4];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                f32x2_t pv;
+                pv[0] = p[w >> 1][2 * (w & 1)];
+                pv[1] = p[w >> 1][2 * (w & 1) + 1];
+#pragma unroll
+                for (int k = 0; k < 3; ++k) {
+                    const uint32_t two = __builtin_bit_cast(uint32_t, __builtin_convertvector(pv, bf16x2_t));
+                    part[k][w] = two;
+                    pv[0] -= __uint_as_float(two << 16);
+                    pv[1] -= __uint_as_float(two & 0xFFFF0000u);
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                uint32_t vt[4];
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    vt[w] = __builtin_amdgcn_perm(x.v[2 * w + 1][c >> 1], x.v[2 * w][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
+                const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(vt[0], vt[1], vt[2], vt[3]));
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+                    acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        vf, __builtin_bit_cast(bf16x8_t, make_uint4(part[k][0], part[k][1], part[k][2], part[k][3])), acc[c], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+                    acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[i][c]), p[0][i], acc[c], 0, 0, 0);
+        }
+        if constexpr (MORE) {
+            load_v(x, t + 4, id);
+#pragma unroll
+            for (int hf = 0; hf < HV; ++hf) id[hf] = id2[hf];
+        }
+    };
+    int t = ta + wave;
+    if (t < tb) {
+        pages_of(t, id);
+        load_k(x, t, id);
+        load_v(x, t, id);
+        pages_of(t + 4, id);
+        for (; t + 4 < tb; t += 4) tile(t, std::true_type());
+        tile(t, std::false_type());
+    }
+
+    // ---- the four waves' parts, through LDS: lane (lq, lj) holds head dimensions 4 C lj .. 4 C (lj + 1) - 1 of query lq
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (lq < gt) {
+        if (lj == 0) {
+            red.m[wave][lq] = m;
+            red.l[wave][lq] = l;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int c = 0; c < C; c += 4)
+                *reinterpret_cast<f32x4_t *>(&red.part[wave][lq][(4 * lj + i) * C + c]) =
+                    f32x4_t{acc[c][i], acc[c + 1][i], acc[c + 2][i], acc[c + 3][i]};
+    }
+    __syncthreads();
+}
+
 template <bool BF16, int D, bool WEIGHTS>
 __global__ void __launch_bounds__(256, 3)
 paged_split(AttendArgs a)
 {
-    using P = Shape<BF16, D>;
-    constexpr int TR = P::TR, RB = P::RB, HV = P::HV, NK = P::NK, C = P::C, VW = P::VW, NV = P::NV;
-    constexpr int LD = D + 4;                            // a row of the merge area: shifts the banks from query to query
-    __shared__ float red[4][kPagedQueries][LD];
-    __shared__ float red_m[4][kPagedQueries], red_l[4][kPagedQueries];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int lq = lane & 15, lj = lane >> 4;
+    constexpr int TR = Shape<BF16, D>::TR;
+    __shared__ Merge<D> red;
+    const int tid = threadIdx.x, lane = tid & 63;
     const int b = blockIdx.x, groups = gridDim.x;
-    const int cap = a.per_seq << a.page_shift, pmask = (1 << a.page_shift) - 1;
+    const int cap = a.per_seq << a.page_shift;
     const int pairs = a.H * a.tiles_q;                   // of one sequence
     const int g = a.Hq / a.H;
 
@@ -149,216 +391,13 @@ paged_split(AttendArgs a)
         const int h = pair / a.tiles_q, q0 = pair % a.tiles_q * kPagedQueries;
         const int gt = min(kPagedQueries, g - q0);
         const long long qrow = (long long)s * a.Hq + h * g + q0;
-        float *logits = a.logits + (WEIGHTS ? ((long long)(s * a.H + h) * logit_rows(cap) * g + q0 * TR) : 0);
-        const scalar_i32 table = as_scalar(a.table) + (long long)s * a.per_seq;
-        const int last16 = (n - 1) & ~15;                // a tile's second half may not exist: it reads this one instead
-
-        // queries: the lane's part of query lq's row, in the order of the K loads; heads that do not exist are zero
-        uint4 qf[NK];
-#pragma unroll
-        for (int kk = 0; kk < NK; ++kk) {
-            qf[kk] = make_uint4(0, 0, 0, 0);
-            if (lq < gt)
-                qf[kk] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(a.Q) + (qrow + lq) * RB + kk * 64 + lj * 16);
-        }
-        auto pages_of = [&](int t, int (&id)[HV]) {
-#pragma unroll
-            for (int hf = 0; hf < HV; ++hf) id[hf] = table[min(t * TR + 16 * hf, last16) >> a.page_shift];
-        };
-        auto half_base = [&](int t, int hf, int id) {    // where half hf of tile t starts in the pools
-            const int r = min(t * TR + 16 * hf, last16);
-            return (unsigned long long)(paged_base(id, a.pages, a.H, h, 1 << a.page_shift) + (r & pmask)) * RB;
-        };
-        const unsigned koff = lq * RB + lj * 16, voff = 4 * lj * RB + lq * VW * 4;
-        auto load_k = [&](Tile<BF16, D> &x, int t, const int (&id)[HV]) {
-#pragma unroll
-            for (int hf = 0; hf < HV; ++hf) {
-                const char *p = reinterpret_cast<const char *>(a.K) + half_base(t, hf, id[hf]);
-#pragma unroll
-                for (int kk = 0; kk < NK; ++kk) x.k[hf][kk] = load16(p + koff + kk * 64);
-            }
-        };
-        auto load_v = [&](Tile<BF16, D> &x, int t, const int (&id)[HV]) {
-#pragma unroll
-            for (int hf = 0; hf < HV; ++hf) {
-                const char *p = reinterpret_cast<const char *>(a.V) + half_base(t, hf, id[hf]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if constexpr (VW == 2) {
-                        typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
-                        const u32x2_t w = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t *>(p + voff + i * RB));
-                        x.v[4 * hf + i][0] = w[0], x.v[4 * hf + i][1] = w[1];
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < VW / 4; ++j) {
-                            const uint4 w = load16(p + voff + i * RB + 16 * j);
-                            x.v[4 * hf + i][4 * j] = w.x, x.v[4 * hf + i][4 * j + 1] = w.y;
-                            x.v[4 * hf + i][4 * j + 2] = w.z, x.v[4 * hf + i][4 * j + 3] = w.w;
-                        }
-                    }
-                }
-            }
-        };
-
-        float m = -__builtin_inff(), l = 0.0f;           // of query lq; l of the lane's rows only
-        f32x4_t acc[C];
-#pragma unroll
-        for (int c = 0; c < C; ++c) acc[c] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-
-        Tile<BF16, D> x;
-        int id[HV];                                      // pages of the tile to load next
-        // One tile, held in x.  MORE: the wave's next tile, t + 4, is loaded behind the last use of K and of V (so one of the two
-        // is always on its way), and the pages of the one after it are looked up; a tile with another one behind it is whole.
-        auto tile = [&](int t, auto more) {
-            constexpr bool MORE = decltype(more)::value;
-            int id2[HV];
-            if constexpr (MORE) pages_of(t + 8, id2);
-            // scores of rows 16 hf + 4 lj + i for query lq
-            f32x4_t z[HV];
-#pragma unroll
-            for (int hf = 0; hf < HV; ++hf) {
-                z[hf] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int kk = 0; kk < NK; ++kk) {
-                    if constexpr (BF16) {
-                        z[hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x.k[hf][kk]),
-                                                                       __builtin_bit_cast(bf16x8_t, qf[kk]), z[hf], 0, 0, 0);
-                    } else {
-                        const uint32_t kw[4] = {x.k[hf][kk].x, x.k[hf][kk].y, x.k[hf][kk].z, x.k[hf][kk].w};
-                        const uint32_t qw[4] = {qf[kk].x, qf[kk].y, qf[kk].z, qf[kk].w};
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            z[hf] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kw[e]), __uint_as_float(qw[e]), z[hf], 0, 0, 0);
-                    }
-                }
-            }
-            if constexpr (MORE) load_k(x, t + 4, id);
-            const int r0 = t * TR + 4 * lj;              // the lane's first row
-            float top = -__builtin_inff();
-#pragma unroll
-            for (int hf = 0; hf < HV; ++hf)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    z[hf][i] *= a.scale_log2;
-                    // rows behind the sequence's last one hold anything: their score is replaced, and so is their V below
-                    if (!MORE && r0 + 16 * hf + i >= n) z[hf][i] = -__builtin_inff();
-                    top = fmaxf(top, z[hf][i]);
-                }
-            if (WEIGHTS && lq < gt) {
-                float *to = logits + ((long long)t * g + lq) * TR + 4 * lj;
-#pragma unroll
-                for (int hf = 0; hf < HV; ++hf)
-                    if (MORE || r0 + 16 * hf < n) *reinterpret_cast<f32x4_t *>(to + 16 * hf) = z[hf];
-            }
-            // the reference is moved only when a score exceeds it by more than 2^8: weights stay far from overflow, and the
-            // accumulator is rescaled a few times per pass instead of once per tile.  (All four lanes of a query agree.)
-            if (__any(top > m + 8.0f)) {
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float to = fmaxf(m, top);
-                const float fade = __builtin_amdgcn_exp2f(m - to);
-                m = to;
-                l *= fade;
-#pragma unroll
-                for (int c = 0; c < C; ++c) acc[c] *= fade;
-            }
-            float p[HV][4];
-#pragma unroll
-            for (int hf = 0; hf < HV; ++hf)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    p[hf][i] = __builtin_amdgcn_exp2f(z[hf][i] - m);
-                    l += p[hf][i];
-                }
-            if constexpr (!MORE) {
-#pragma unroll
-                for (int e = 0; e < NV; ++e)
-#pragma unroll
-                    for (int w = 0; w < VW; ++w) x.v[e][w] = r0 + (e >> 2) * 16 + (e & 3) >= n ? 0u : x.v[e][w];
-            }
-            // O^T += V^T P^T
-            if constexpr (BF16) {
-                // a weight as the sum of three bf16 numbers, all its 24 bits: one alone would cost 2^-9 of it, two 2^-17, which
-                // shows in the output (the matrix cores have the time)
-                uint32_t part[3][4];
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    f32x2_t pv;
-                    pv[0] = p[w >> 1][2 * (w & 1)];
-                    pv[1] = p[w >> 1][2 * (w & 1) + 1];
-#pragma unroll
-                    for (int k = 0; k < 3; ++k) {
-                        const uint32_t two = __builtin_bit_cast(uint32_t, __builtin_convertvector(pv, bf16x2_t));
-                        part[k][w] = two;
-                        pv[0] -= __uint_as_float(two << 16);
-                        pv[1] -= __uint_as_float(two & 0xFFFF0000u);
-                    }
-                }
-#pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    uint32_t vt[4];
-#pragma unroll
-                    for (int w = 0; w < 4; ++w)
-                        vt[w] = __builtin_amdgcn_perm(x.v[2 * w + 1][c >> 1], x.v[2 * w][c >> 1], c & 1 ? 0x07060302u : 0x05040100u);
-                    const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(vt[0], vt[1], vt[2], vt[3]));
-#pragma unroll
-                    for (int k = 0; k < 3; ++k)
-                        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            vf, __builtin_bit_cast(bf16x8_t, make_uint4(part[k][0], part[k][1], part[k][2], part[k][3])), acc[c], 0, 0, 0);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int c = 0; c < C; ++c)
-                        acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[i][c]), p[0][i], acc[c], 0, 0, 0);
-            }
-            if constexpr (MORE) {
-                load_v(x, t + 4, id);
-#pragma unroll
-                for (int hf = 0; hf < HV; ++hf) id[hf] = id2[hf];
-            }
-        };
-        int t = ta + wave;
-        if (t < tb) {
-            pages_of(t, id);
-            load_k(x, t, id);
-            load_v(x, t, id);
-            pages_of(t + 4, id);
-            for (; t + 4 < tb; t += 4) tile(t, std::true_type());
-            tile(t, std::false_type());
-        }
-
-        // ---- the four waves' parts, through LDS: lane (lq, lj) holds head dimensions 4 C lj .. 4 C (lj + 1) - 1 of query lq
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        if (lq < gt) {
-            if (lj == 0) {
-                red_m[wave][lq] = m;
-                red_l[wave][lq] = l;
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int c = 0; c < C; c += 4)
-                    *reinterpret_cast<f32x4_t *>(&red[wave][lq][(4 * lj + i) * C + c]) =
-                        f32x4_t{acc[c][i], acc[c + 1][i], acc[c + 2][i], acc[c + 3][i]};
-        }
-        __syncthreads();
+        sweep<BF16, D, WEIGHTS ? kToMemory : kNowhere>(a, s, h, q0, n, ta, tb, red, nullptr, 0);
         const bool all = ta == 0 && tb == ts;            // nobody else has a part of this pair
         const int slot = 2 * b + (t0 == run0 ? 0 : 1);
         for (int i = tid; i < gt * D; i += 256) {
             const int q = i / D, e = i % D;
-            float top = red_m[0][q];
-#pragma unroll
-            for (int w = 1; w < 4; ++w) top = fmaxf(top, red_m[w][q]);
-            float sum = 0.0f, lsum = 0.0f;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const float f = __builtin_amdgcn_exp2f(red_m[w][q] - top);
-                sum = fmaf(red[w][q][e], f, sum);
-                lsum = fmaf(red_l[w][q], f, lsum);
-            }
+            float top, lsum, sum;
+            red.query(q, e, top, lsum, sum);
             if (all) {
                 a.O[(qrow + q) * D + e] = sum / lsum;
                 if (e == 0) {
@@ -378,6 +417,72 @@ paged_split(AttendArgs a)
         if (ta == 0 && tid == 0) a.start[(long long)s * pairs + pair] = pair0;
         __syncthreads();
         t0 = pair0 + tb;
+    }
+}
+
+// decay * mass_in + w of four rows, to mass_out.
+__device__ __forceinline__ void account(const AttendArgs &a, long long at, int r, int n, const f32x4_t &w)
+{
+    at += r;
+    if (r + 4 <= n && a.aligned) {
+        f32x4_t x = w;
+        if (a.mass_in != nullptr) {
+            const f32x4_t old = *reinterpret_cast<const f32x4_t *>(a.mass_in + at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = fmaf(a.decay, old[i], w[i]);
+        }
+        *reinterpret_cast<f32x4_t *>(a.mass_out + at) = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (r + i < n) a.mass_out[at + i] = a.mass_in != nullptr ? fmaf(a.decay, a.mass_in[at + i], w[i]) : w[i];
+    }
+}
+
+// Short caches: one workgroup has all rows of its (sequence, KV head, query heads), so nothing is left to join, and the logits, kept
+// in LDS, become weights in the same launch.
+template <bool BF16, int D, bool WEIGHTS>
+__global__ void __launch_bounds__(256, 3)
+paged_whole(AttendArgs a, int kept_stride)
+{
+    constexpr int TR = Shape<BF16, D>::TR;
+    __shared__ Merge<D> red;
+    __shared__ float stat[kPagedQueries];
+    extern __shared__ float kept[];                      // [g][kept_stride] logits
+    const int tid = threadIdx.x;
+    const int cap = a.per_seq << a.page_shift, g = a.Hq / a.H;
+    const int qt = blockIdx.x % a.tiles_q, pair = blockIdx.x / a.tiles_q, s = pair / a.H, h = pair % a.H;
+    const int q0 = qt * kPagedQueries, gt = min(kPagedQueries, g - q0);
+    const int n = paged_rows(as_scalar(a.len)[s], cap);
+    const long long qrow = (long long)s * a.Hq + h * g + q0;
+    if (n == 0) {
+        for (int i = tid; i < gt * D; i += 256) a.O[qrow * D + i] = 0.0f;
+        if (tid < gt && a.lse != nullptr) a.lse[qrow + tid] = -__builtin_inff();
+        return;
+    }
+    sweep<BF16, D, WEIGHTS ? kToLds : kNowhere>(a, s, h, q0, n, 0, (n + TR - 1) / TR, red, kept, kept_stride);
+    for (int i = tid; i < gt * D; i += 256) {
+        const int q = i / D, e = i % D;
+        float top, lsum, sum;
+        red.query(q, e, top, lsum, sum);
+        a.O[(qrow + q) * D + e] = sum / lsum;
+        if (e == 0) {
+            const float z = top + __builtin_amdgcn_logf(lsum);
+            stat[q] = z;
+            if (a.lse != nullptr) a.lse[qrow + q] = z * 0.693147180559945309f;
+        }
+    }
+    if constexpr (WEIGHTS) {
+        __syncthreads();
+        for (int r = tid * 4; r < n; r += 1024) {
+            f32x4_t w = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int q = 0; q < gt; ++q) {
+                const f32x4_t z = *reinterpret_cast<const f32x4_t *>(kept + q * kept_stride + r);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] += __builtin_amdgcn_exp2f(z[i] - stat[q]);
+            }
+            account(a, (long long)pair * cap, r, n, w);
+        }
     }
 }
 
@@ -460,8 +565,8 @@ __device__ void add_weights(const AttendArgs &a, int groups, int pair, int chunk
     const int n = paged_rows(a.len[s], cap);
     if (chunk * 1024 >= n) return;
     const int r = chunk * 1024 + tid * 4;
-    const float *z = a.logits + ((long long)pair * logit_rows(cap) + r / TR * TR) * g + r % TR;
-    float w[4] = {};
+    const float *z = a.logits + ((long long)pair * logit_rows(cap) + r / 16 * 16) * g + r % 16;
+    f32x4_t w = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int q0 = 0; q0 < g; q0 += 256) {
         if (q0 > 0) __syncthreads();
         // the sum of all weights of query head q, log2: as written by the one workgroup that had it all, or from its parts
@@ -485,27 +590,13 @@ __device__ void add_weights(const AttendArgs &a, int groups, int pair, int chunk
         if (r < n)
 #pragma unroll 4
             for (int q = q0; q < min(g, q0 + 256); ++q) {
-                const f32x4_t x = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t *>(z + (long long)q * TR));
+                const f32x4_t x = __builtin_nontemporal_load(reinterpret_cast<const f32x4_t *>(z + (long long)q * 16));
                 const float all = stat[q - q0];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w[i] += __builtin_amdgcn_exp2f(x[i] - all);
             }
     }
-    if (r >= n) return;
-    const long long at = (long long)pair * cap + r;
-    if (r + 4 <= n && a.aligned) {
-        f32x4_t x = {w[0], w[1], w[2], w[3]};
-        if (a.mass_in != nullptr) {
-            const f32x4_t old = *reinterpret_cast<const f32x4_t *>(a.mass_in + at);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = fmaf(a.decay, old[i], w[i]);
-        }
-        *reinterpret_cast<f32x4_t *>(a.mass_out + at) = x;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (r + i < n) a.mass_out[at + i] = a.mass_in != nullptr ? fmaf(a.decay, a.mass_in[at + i], w[i]) : w[i];
-    }
+    if (r < n) account(a, (long long)pair * cap, r, n, w);
 }
 
 template <bool BF16, int D>
@@ -545,6 +636,13 @@ hipError_t launch_paged_attend(const ws_paged_cache &c, const void *Q, int Hq, f
         constexpr bool B = decltype(BF)::value;
         constexpr int D = decltype(DD)::value;
         const dim3 grid((unsigned)groups), block(256);
+        if (paged_whole_heads(c.S, c.Hkv, Hq, cap, mass_out != nullptr)) {
+            const dim3 heads((unsigned)(c.S * c.Hkv * a.tiles_q));
+            const int stride = mass_out ? logit_rows(cap) + 4 : 0;
+            if (mass_out) hipLaunchKernelGGL((paged_whole<B, D, true>), heads, block, stride * (Hq / c.Hkv) * sizeof(float), st, a, stride);
+            else hipLaunchKernelGGL((paged_whole<B, D, false>), heads, block, 0, st, a, stride);
+            return hipGetLastError();
+        }
         if (mass_out) hipLaunchKernelGGL((paged_split<B, D, true>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((paged_split<B, D, false>), grid, block, 0, st, a);
         const hipError_t e = hipGetLastError();

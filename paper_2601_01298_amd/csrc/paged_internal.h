@@ -28,6 +28,22 @@ static inline int paged_groups(bool bf16, int S, int Hkv, int Hq, int cap)
 // whole tiles of logits per query head
 __host__ __device__ static inline int logit_rows(int cap) { return (cap + 31) / 32 * 32; }
 
+// their offsets within a head travel in 32 bits
+static inline bool paged_logits_fit(int g, int cap) { return (long long)logit_rows(cap) * g < (1LL << 29); }
+
+// Whether every (sequence, KV head) goes to one workgroup that does all of it.
+constexpr int kWholeLogits = 5120;          // logits it keeps in LDS: 20 KB beside the merge area
+#ifndef WHOLE_PAIRS
+#define WHOLE_PAIRS 512
+#define WHOLE_ROWS 512
+#endif
+static inline bool paged_whole_heads(int S, int Hkv, int Hq, int cap, bool weights)
+{
+    const int g = Hq / Hkv;
+    if (weights && (g > kPagedQueries || (long long)(logit_rows(cap) + 4) * g > kWholeLogits)) return false;
+    return cap <= WHOLE_ROWS || ((long long)S * Hkv >= WHOLE_PAIRS && cap <= kWholeLogits);
+}
+
 struct PagedAttendSpace {
     size_t start, stats, slot_stats, slots, logits, bytes;   // offsets, total; the first 256 bytes hold the number of tiles
 };
