@@ -1,32 +1,53 @@
 // Eviction by accumulated attention weight.
 //
-// evict_pick: one workgroup per KV head of a sequence.  Every row's account becomes a 32-bit number that orders like it (protected
-// rows above all); the keep-th largest is found digit by digit from the top (counts of the 256 values of a digit among the rows
-// that agree so far), then one ordered pass tells who stays, who of those has to move (it lies at `keep` or behind) and which
-// rows became free, and writes the accounts and stamps.  evict_move: copies the rows of K and V from and to where evict_pick says.
+// Every row's account becomes a 32-bit key that orders like it (protected rows above all numbers, a NaN below).  The keep-th
+// largest key of a head is found in three digits from the top, 11, 11 and 10 bits: count the values of a digit among the keys
+// that agree so far, and take the value at which the counts from above reach what is left to keep.  Who has a larger key
+// stays, and of equal ones the lowest rows; then the rows that became free below `keep` and those that stay behind it are
+// listed in order, and row i of one list goes to row i of the other.
+//
+//   evict_pick   one workgroup per head, keys in registers: up to kPickRows rows.  With few moves it makes them too.
+//   evict_digit (three times), evict_count, evict_place   the same over workgroups of kChunk rows each, for longer heads: a step
+//                that needs all chunks of a head (the counts of a digit, the rows listed before a chunk's) starts with a new
+//                launch and adds up what the chunks left, so nothing waits inside a kernel and nothing is added atomically
+//                between workgroups.
+//   evict_move   copies the rows of K and V, accounts and stamps from and to where the lists say.
+// Bound: HBM (the moved rows); for short heads the chain of barriers of evict_pick.
 #include "paged_internal.h"
 
 namespace ws {
 
 namespace {
 
-constexpr int kPick = 1024;
+constexpr int kDigits[3] = {11, 11, 10};
+constexpr int kBins = 2048;                 // room for a digit's counts
 
 struct EvictArgs {
     void *K, *V;
     const int32_t *table, *len;
-    int pages, H, page, S, per_seq, row_bytes;
+    int pages, H, page_shift, S, per_seq, row_bytes;
     int keep, sinks, recent;
     const int32_t *seen, *stamp_in;
     const float *mass_in;
     float *mass_out;
     int32_t *stamp_out, *len_out, *kept;
-    int32_t *count, *moves;      // [pairs], [pairs][2][most]
-    int most;
+    int32_t *count, *moves;                 // [pairs], [pairs][2][most]
+    int most, chunks;
+    uint32_t *keys;                         // [pairs][cap]
+    uint16_t *hist;                         // [3][pairs][chunks][kBins]
+    uint2 *cells;                           // [3][pairs]: the digits found so far, and how many rows with exactly them are kept
+    int2 *chunk_stays;                      // [pairs][chunks]: rows that stay, below `keep` and behind it
+    unsigned long long *bits;               // [pairs][chunks][kChunk / 64]: who stays
+    __device__ int rows_of(int s) const { return paged_rows(len[s], per_seq << page_shift); }
+    __device__ int cap() const { return per_seq << page_shift; }
+    __device__ uint16_t *hist_of(int digit, int pair, int chunk) const
+    {
+        return hist + (((long long)digit * S * H + pair) * chunks + chunk) * kBins;
+    }
 };
 
 // Orders as the accounts do: NaN least, protected rows above all numbers.
-__device__ __forceinline__ uint32_t rank_of(float mass, int stamp, int sinks, long long fresh)
+__device__ __forceinline__ uint32_t key_of(float mass, int stamp, int sinks, long long fresh)
 {
     if (stamp < sinks || stamp >= fresh) return 0xFFFFFFFFu;
     if (mass != mass) return 0u;
@@ -34,114 +55,443 @@ __device__ __forceinline__ uint32_t rank_of(float mass, int stamp, int sinks, lo
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// Exclusive sum over the workgroup of v; `total` is the whole.  Two barriers.
-__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t *wave_sum, uint32_t &total)
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v)       // inclusive
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t x = v;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t y = __shfl_up(x, o);
-        if (lane >= o) x += y;
+        const uint32_t y = __shfl_up(v, o);
+        if ((int)(threadIdx.x & 63) >= o) v += y;
     }
-    if (lane == 63) wave_sum[wave] = x;
-    __syncthreads();
-    uint32_t before = 0, all = 0;
-    for (int w = 0; w < kPick / 64; ++w) {
-        const uint32_t c = wave_sum[w];
-        if (w < wave) before += c;
-        all += c;
-    }
-    __syncthreads();
-    total = all;
-    return before + x - v;
+    return v;
 }
 
-__global__ void __launch_bounds__(kPick)
-evict_pick(EvictArgs a)
+__device__ __forceinline__ int below(unsigned long long mask)   // set bits of lower lanes
 {
-    __shared__ uint32_t hist[256];
-    __shared__ uint32_t wave_sum[kPick / 64];
-    __shared__ uint32_t found[2];
-    const int tid = threadIdx.x, pair = blockIdx.x, s = pair / a.H;
-    const int cap = a.per_seq * a.page;
-    const int n = paged_rows(a.len[s], cap);
-    const float *mass = a.mass_in + (long long)pair * cap;
-    const int32_t *stamp = a.stamp_in + (long long)pair * cap;
-    float *mass_out = a.mass_out + (long long)pair * cap;
-    int32_t *stamp_out = a.stamp_out + (long long)pair * cap;
-    int32_t *kept = a.kept != nullptr ? a.kept + (long long)pair * a.keep : nullptr;
-    if (n <= a.keep) {
-        if (tid == 0) a.count[pair] = 0;
-        for (int i = tid; i < n; i += kPick) {
-            mass_out[i] = mass[i];
-            stamp_out[i] = stamp[i];
-            if (kept != nullptr) kept[i] = i;
-        }
-        return;
-    }
-    const long long fresh = (long long)a.seen[s] - a.recent;
-    uint32_t prefix = 0, left = (uint32_t)a.keep;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
-        __syncthreads();
-        const uint32_t known = shift == 24 ? 0u : 0xFFFFFFFFu << (shift + 8);
-        for (int i = tid; i < n; i += kPick) {
-            const uint32_t key = rank_of(mass[i], stamp[i], a.sinks, fresh);
-            if ((key & known) == prefix) atomicAdd(&hist[(key >> shift) & 255], 1u);
-        }
-        __syncthreads();
-        // thread t < 256 holds digit 255 - t, so that sums run from the largest down
-        const uint32_t c = tid < 256 ? hist[255 - tid] : 0u;
-        uint32_t total;
-        const uint32_t above = block_scan(c, wave_sum, total);
-        if (tid < 256 && above < left && left <= above + c) {
-            found[0] = 255 - tid;
-            found[1] = above;
-        }
-        __syncthreads();
-        prefix |= found[0] << shift;
-        left -= found[1];
-        __syncthreads();
-    }
-    // rows above the threshold stay, and of those at it the first `left`
-    int32_t *free_rows = a.moves + (long long)pair * 2 * a.most, *movers = free_rows + a.most;
-    uint32_t ties = 0, nfree = 0, nmove = 0;
-    for (int i0 = 0; i0 < n; i0 += kPick) {
-        const int i = i0 + tid;
-        float m = 0.0f;
-        int st = 0;
-        uint32_t key = 0;
-        if (i < n) {
-            m = mass[i];
-            st = stamp[i];
-            key = rank_of(m, st, a.sinks, fresh);
-        }
-        const bool tie = i < n && key == prefix;
-        uint32_t total;
-        const uint32_t rank = block_scan(tie ? 1u : 0u, wave_sum, total);
-        const bool stays = i < n && (key > prefix || (tie && ties + rank < left));
-        ties += total;
-        const bool hole = i < n && i < a.keep && !stays, mover = stays && i >= a.keep;
-        const uint32_t at = block_scan((hole ? 1u : 0u) | (mover ? 0x10000u : 0u), wave_sum, total);
-        if (hole) free_rows[nfree + (at & 0xFFFFu)] = i;
-        if (mover) movers[nmove + (at >> 16)] = i;
-        nfree += total & 0xFFFFu;
-        nmove += total >> 16;
-        if (stays && i < a.keep) {
-            mass_out[i] = m;
-            stamp_out[i] = st;
-            if (kept != nullptr) kept[i] = i;
-        }
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+// The digit at which counts from the largest value down reach `left`.  Thread t holds PER counts, of the values PER (THREADS - 1 - t)
+// and up.  Returned to all: the digit, and `left` less what lies above it.  Two barriers.
+template <int THREADS, int PER>
+__device__ __forceinline__ int find_digit(const uint32_t (&c)[PER], uint32_t &left, uint32_t *wave_sum, uint32_t *found)
+{
+    const int tid = threadIdx.x;
+    uint32_t mine = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) mine += c[i];
+    const uint32_t upto = wave_scan(mine);
+    if ((tid & 63) == 63) wave_sum[tid >> 6] = upto;
+    __syncthreads();
+    uint32_t above = upto - mine;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64 - 1; ++w)
+        if (w < tid >> 6) above += wave_sum[w];
+    if (above < left && left <= above + mine) {
+        int i = PER - 1;
+        while (above + c[i] < left) above += c[i--];
+        found[0] = PER * (THREADS - 1 - tid) + i;
+        found[1] = left - above;
     }
     __syncthreads();
-    for (uint32_t j = tid; j < nfree; j += kPick) {
-        const int to = free_rows[j], from = movers[j];
-        mass_out[to] = mass[from];
-        stamp_out[to] = stamp[from];
-        if (kept != nullptr) kept[to] = from;
+    left = found[1];
+    return (int)found[0];
+}
+
+// Copies move j .. of a head with the threads of a group of `pieces`: rows of K and V 16 bytes a thread, U moves at a time, and by the
+// first thread the account, the stamp and the note of where the row came from.
+template <int U>
+__device__ __forceinline__ void move_rows(const EvictArgs &a, int pair, const int32_t *free_rows, const int32_t *movers, int count, int group,
+                                          int groups, int piece)
+{
+    const int s = pair / a.H, h = pair % a.H, pmask = (1 << a.page_shift) - 1;
+    const int32_t *table = a.table + (long long)s * a.per_seq;
+    const long long at = (long long)pair * a.cap();
+    for (int j0 = group; j0 < count; j0 += groups * U) {
+        int to[U], from[U], to_page[U], from_page[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int j = min(j0 + u * groups, count - 1);
+            to[u] = free_rows[j];
+            from[u] = movers[j];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            to_page[u] = table[to[u] >> a.page_shift];
+            from_page[u] = table[from[u] >> a.page_shift];
+        }
+        uint4 k[U], v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long src = (paged_base(from_page[u], a.pages, a.H, h, 1 << a.page_shift) + (from[u] & pmask)) * a.row_bytes + piece * 16;
+            k[u] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(a.K) + src);
+            v[u] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(a.V) + src);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (j0 + u * groups >= count) break;
+            if ((unsigned)to_page[u] < (unsigned)a.pages) {
+                const long long dst = (paged_base(to_page[u], a.pages, a.H, h, 1 << a.page_shift) + (to[u] & pmask)) * a.row_bytes + piece * 16;
+                *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(a.K) + dst) = k[u];
+                *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(a.V) + dst) = v[u];
+            }
+            if (piece == 0) {
+                a.mass_out[at + to[u]] = a.mass_in[at + from[u]];
+                a.stamp_out[at + to[u]] = a.stamp_in[at + from[u]];
+                if (a.kept != nullptr) a.kept[(long long)pair * a.keep + to[u]] = from[u];
+            }
+        }
     }
-    if (tid == 0) a.count[pair] = (int)nfree;
+}
+
+// A row that stays where it is: its account and stamp where they are wanted elsewhere.
+__device__ __forceinline__ void leave_row(const EvictArgs &a, int pair, int i)
+{
+    const long long at = (long long)pair * a.cap() + i;
+    if (a.mass_out != a.mass_in) a.mass_out[at] = a.mass_in[at];
+    if (a.stamp_out != a.stamp_in) a.stamp_out[at] = a.stamp_in[at];
+    if (a.kept != nullptr) a.kept[(long long)pair * a.keep + i] = i;
+}
+
+constexpr int kInlineMoves = 128;           // moves of a head that evict_pick makes itself
+
+// Wave w has rows 64 KPT w and up, KPT runs of 64: the order of rows is the order of waves, runs and lanes.
+template <int THREADS, int KPT, bool MOVE>
+__global__ void __launch_bounds__(THREADS)
+evict_pick(EvictArgs a)
+{
+    constexpr int WAVES = THREADS / 64;
+    __shared__ uint32_t hist[3][kBins];
+    __shared__ uint32_t wave_sum[WAVES], found[2];
+    __shared__ int wave_ties[WAVES], wave_free[WAVES], wave_move[WAVES];
+    __shared__ int32_t lists[2][MOVE ? kInlineMoves : 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int pair = blockIdx.x, s = pair / a.H;
+    const int n = a.rows_of(s);
+    if (MOVE && pair % a.H == 0 && tid == 0 && a.len_out != a.len) a.len_out[s] = min(n, a.keep);
+    const int row0 = wave * 64 * KPT + lane;
+    if (n <= a.keep) {
+        if (!MOVE && tid == 0) a.count[pair] = 0;
+#pragma unroll 4
+        for (int k = 0; k < KPT; ++k)
+            if (row0 + k * 64 < n) leave_row(a, pair, row0 + k * 64);
+        return;
+    }
+    const long long at = (long long)pair * a.cap(), fresh = (long long)a.seen[s] - a.recent;
+    float mass[KPT];
+    int stamp[KPT];
+#pragma unroll
+    for (int k = 0; k < KPT; ++k) {
+        const int i = min(row0 + k * 64, n - 1);
+        mass[k] = a.mass_in[at + i];
+        stamp[k] = a.stamp_in[at + i];
+    }
+    for (int i = tid; i < 3 * kBins; i += THREADS) (&hist[0][0])[i] = 0;
+    __syncthreads();
+    uint32_t key[KPT];
+#pragma unroll
+    for (int k = 0; k < KPT; ++k) key[k] = key_of(mass[k], stamp[k], a.sinks, fresh);
+    uint32_t prefix = 0, left = (uint32_t)a.keep;
+    int shift = 32;
+#pragma unroll
+    for (int digit = 0; digit < 3; ++digit) {
+        const uint32_t known = digit == 0 ? 0u : 0xFFFFFFFFu << shift;
+        shift -= kDigits[digit];
+#pragma unroll
+        for (int k = 0; k < KPT; ++k)
+            if (row0 + k * 64 < n && (key[k] & known) == prefix) atomicAdd(&hist[digit][(key[k] >> shift) & ((1 << kDigits[digit]) - 1)], 1u);
+        __syncthreads();
+        constexpr int PER = kBins / THREADS;
+        uint32_t c[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) c[i] = hist[digit][PER * (THREADS - 1 - tid) + i];
+        prefix |= (uint32_t)find_digit<THREADS, PER>(c, left, wave_sum, found) << shift;
+    }
+    // rows with a larger key stay, and of those with this one the first `left`
+    int ties = 0;
+#pragma unroll
+    for (int k = 0; k < KPT; ++k) ties += __popcll(__ballot(row0 + k * 64 < n && key[k] == prefix));
+    if (lane == 0) wave_ties[wave] = ties;
+    __syncthreads();
+    ties = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES - 1; ++w)
+        if (w < wave) ties += wave_ties[w];
+    uint32_t stays = 0;                                          // bit k: row k of this lane
+    int nfree = 0, nmove = 0;
+#pragma unroll
+    for (int k = 0; k < KPT; ++k) {
+        const int i = row0 + k * 64;
+        const bool tie = i < n && key[k] == prefix;
+        const unsigned long long mask = __ballot(tie);
+        const bool stay = i < n && (key[k] > prefix || (tie && ties + below(mask) < (int)left));
+        ties += __popcll(mask);
+        if (stay) stays |= 1u << k;
+        nfree += __popcll(__ballot(i < a.keep && !stay));
+        nmove += __popcll(__ballot(i >= a.keep && stay));
+    }
+    if (lane == 0) {
+        wave_free[wave] = nfree;
+        wave_move[wave] = nmove;
+    }
+    __syncthreads();
+    int all = 0;
+    nfree = nmove = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) {
+            nfree += wave_free[w];
+            nmove += wave_move[w];
+        }
+        all += wave_free[w];
+    }
+    int32_t *free_rows = MOVE ? lists[0] : a.moves + (long long)pair * 2 * a.most, *movers = MOVE ? lists[1] : free_rows + a.most;
+#pragma unroll
+    for (int k = 0; k < KPT; ++k) {
+        const int i = row0 + k * 64;
+        const bool stay = (stays >> k) & 1u, is_free = i < a.keep && !stay, moves = i >= a.keep && stay;
+        const unsigned long long fm = __ballot(is_free), mm = __ballot(moves);
+        if (is_free) free_rows[nfree + below(fm)] = i;
+        if (moves) movers[nmove + below(mm)] = i;
+        nfree += __popcll(fm);
+        nmove += __popcll(mm);
+        if (stay && !moves) leave_row(a, pair, i);
+    }
+    if constexpr (MOVE) {
+        __syncthreads();
+        const int pieces = a.row_bytes / 16;
+        move_rows<2>(a, pair, free_rows, movers, all, tid / pieces, THREADS / pieces, tid % pieces);
+    } else {
+        if (tid == 0) a.count[pair] = all;
+    }
+}
+
+__global__ void __launch_bounds__(256)
+evict_lengths(EvictArgs a)
+{
+    const int s = blockIdx.x * 256 + threadIdx.x;
+    if (s < a.S) a.len_out[s] = min(a.rows_of(s), a.keep);
+}
+
+// ---- heads of more rows: a workgroup per chunk ------------------------------------------------------------------------------
+constexpr int kChunkKeys = kChunk / 256;    // per thread
+
+__device__ __forceinline__ int chunk_row(int chunk, int k) { return chunk * kChunk + (threadIdx.x >> 6) * (kChunk / 4) + k * 64 + (threadIdx.x & 63); }
+
+// The value of digit `d` from the counts that all chunks of the head left; `left` as in find_digit.
+template <int BINS>
+__device__ __forceinline__ int digit_of_chunks(const EvictArgs &a, int d, int pair, int chunks, uint32_t &left, uint32_t *wave_sum, uint32_t *found)
+{
+    constexpr int PER = BINS / 256;
+    const uint16_t *h = a.hist_of(d, pair, 0) + PER * (255 - (int)threadIdx.x);
+    uint32_t c[PER] = {};
+#pragma unroll 8
+    for (int i = 0; i < chunks; ++i) {
+        uint32_t w[PER / 2];
+        if constexpr (PER == 8) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(h + (long long)i * kBins);
+            w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+        } else {
+            const uint2 x = *reinterpret_cast<const uint2 *>(h + (long long)i * kBins);
+            w[0] = x.x, w[1] = x.y;
+        }
+#pragma unroll
+        for (int j = 0; j < PER / 2; ++j) {
+            c[2 * j] += w[j] & 0xFFFFu;
+            c[2 * j + 1] += w[j] >> 16;
+        }
+    }
+    return find_digit<256, PER>(c, left, wave_sum, found);
+}
+
+template <int DIGIT>
+__global__ void __launch_bounds__(256)
+evict_digit(EvictArgs a)
+{
+    __shared__ uint32_t hist[kBins];
+    __shared__ uint32_t wave_sum[4], found[2];
+    const int tid = threadIdx.x, chunk = blockIdx.x, pair = blockIdx.y + blockIdx.z * gridDim.y;
+    if (pair >= a.S * a.H) return;
+    const int n = a.rows_of(pair / a.H), chunks = (n + kChunk - 1) / kChunk;
+    if (chunk >= chunks) return;
+    if (n <= a.keep) {
+        if (DIGIT == 0)
+            for (int k = 0; k < kChunkKeys; ++k)
+                if (chunk_row(chunk, k) < n) leave_row(a, pair, chunk_row(chunk, k));
+        return;
+    }
+    const long long at = (long long)pair * a.cap();
+    uint32_t key[kChunkKeys];
+    if constexpr (DIGIT == 0) {
+        const long long fresh = (long long)a.seen[pair / a.H] - a.recent;
+        float mass[kChunkKeys];
+        int stamp[kChunkKeys];
+#pragma unroll
+        for (int k = 0; k < kChunkKeys; ++k) {
+            const int i = min(chunk_row(chunk, k), n - 1);
+            mass[k] = a.mass_in[at + i];
+            stamp[k] = a.stamp_in[at + i];
+        }
+#pragma unroll
+        for (int k = 0; k < kChunkKeys; ++k) key[k] = key_of(mass[k], stamp[k], a.sinks, fresh);
+    } else {
+#pragma unroll
+        for (int k = 0; k < kChunkKeys; ++k) key[k] = a.keys[at + min(chunk_row(chunk, k), n - 1)];
+    }
+    for (int i = tid; i < kBins; i += 256) hist[i] = 0;
+    uint32_t prefix = 0, left = (uint32_t)a.keep;
+    if constexpr (DIGIT > 0) {
+        if constexpr (DIGIT == 2) {
+            const uint2 cell = a.cells[pair];
+            prefix = cell.x, left = cell.y;
+        }
+        prefix |= (uint32_t)digit_of_chunks<kBins>(a, DIGIT - 1, pair, chunks, left, wave_sum, found) << (DIGIT == 1 ? 21 : 10);
+        if (chunk == 0 && tid == 0) a.cells[(long long)(DIGIT - 1) * a.S * a.H + pair] = make_uint2(prefix, left);
+    }
+    __syncthreads();
+    constexpr int SHIFT = DIGIT == 0 ? 21 : DIGIT == 1 ? 10 : 0;
+    constexpr uint32_t KNOWN = DIGIT == 0 ? 0u : DIGIT == 1 ? 0xFFFFFFFFu << 21 : 0xFFFFFFFFu << 10;
+#pragma unroll
+    for (int k = 0; k < kChunkKeys; ++k)
+        if (chunk_row(chunk, k) < n) {
+            if (DIGIT == 0) a.keys[at + chunk_row(chunk, k)] = key[k];
+            if ((key[k] & KNOWN) == prefix) atomicAdd(&hist[(key[k] >> SHIFT) & ((1 << kDigits[DIGIT]) - 1)], 1u);
+        }
+    __syncthreads();
+    uint32_t *out = reinterpret_cast<uint32_t *>(a.hist_of(DIGIT, pair, chunk));
+    for (int i = tid; i < (1 << kDigits[DIGIT]) / 2; i += 256) out[i] = hist[2 * i] | hist[2 * i + 1] << 16;
+}
+
+// Who stays: one bit per row, and how many per chunk.
+__global__ void __launch_bounds__(256)
+evict_count(EvictArgs a)
+{
+    __shared__ uint32_t wave_sum[4], found[2];
+    __shared__ int wave_ties[4], wave_stays[2][4], before;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, chunk = blockIdx.x, pair = blockIdx.y + blockIdx.z * gridDim.y;
+    if (pair >= a.S * a.H) return;
+    const int n = a.rows_of(pair / a.H), chunks = (n + kChunk - 1) / kChunk;
+    if (chunk >= chunks || n <= a.keep) return;
+    const long long at = (long long)pair * a.cap();
+    uint32_t key[kChunkKeys];
+#pragma unroll
+    for (int k = 0; k < kChunkKeys; ++k) key[k] = a.keys[at + min(chunk_row(chunk, k), n - 1)];
+    const uint2 cell = a.cells[(long long)a.S * a.H + pair];
+    uint32_t left = cell.y;
+    const int digit = digit_of_chunks<kBins / 2>(a, 2, pair, chunks, left, wave_sum, found);
+    const uint32_t prefix = cell.x | (uint32_t)digit;
+    // equal keys in the chunks before this one
+    if (wave == 0) {
+        int sum = 0;
+        for (int c = lane; c < chunk; c += 64) sum += a.hist_of(2, pair, c)[digit];
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+        if (lane == 0) before = sum;
+    }
+    int ties = 0;
+#pragma unroll
+    for (int k = 0; k < kChunkKeys; ++k) ties += __popcll(__ballot(chunk_row(chunk, k) < n && key[k] == prefix));
+    if (lane == 0) wave_ties[wave] = ties;
+    __syncthreads();
+    ties = before;
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+        if (w < wave) ties += wave_ties[w];
+    int low = 0, high = 0;
+#pragma unroll
+    for (int k = 0; k < kChunkKeys; ++k) {
+        const int i = chunk_row(chunk, k);
+        const bool tie = i < n && key[k] == prefix;
+        const unsigned long long mask = __ballot(tie);
+        const bool stay = i < n && (key[k] > prefix || (tie && ties + below(mask) < (int)left));
+        ties += __popcll(mask);
+        const unsigned long long stays = __ballot(stay);
+        if (lane == 0) a.bits[((long long)pair * a.chunks + chunk) * (kChunk / 64) + wave * kChunkKeys + k] = stays;
+        low += __popcll(__ballot(stay && i < a.keep));
+        high += __popcll(__ballot(stay && i >= a.keep));
+    }
+    if (lane == 0) {
+        wave_stays[0][wave] = low;
+        wave_stays[1][wave] = high;
+    }
+    __syncthreads();
+    if (tid == 0)
+        a.chunk_stays[(long long)pair * a.chunks + chunk] =
+            make_int2(wave_stays[0][0] + wave_stays[0][1] + wave_stays[0][2] + wave_stays[0][3],
+                      wave_stays[1][0] + wave_stays[1][1] + wave_stays[1][2] + wave_stays[1][3]);
+}
+
+// The lists of free rows and of rows that move, in order, and the accounts of those that neither are.
+__global__ void __launch_bounds__(256)
+evict_place(EvictArgs a)
+{
+    __shared__ int wave_free[4], wave_move[4], start[3];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, chunk = blockIdx.x, pair = blockIdx.y + blockIdx.z * gridDim.y;
+    if (pair >= a.S * a.H) return;
+    const int n = a.rows_of(pair / a.H), chunks = (n + kChunk - 1) / kChunk;
+    if (n <= a.keep) {
+        if (chunk == 0 && tid == 0) a.count[pair] = 0;
+        return;
+    }
+    if (chunk >= chunks) return;
+    const unsigned long long *bits = a.bits + ((long long)pair * a.chunks + chunk) * (kChunk / 64) + wave * kChunkKeys;
+    unsigned long long mask[kChunkKeys];
+#pragma unroll
+    for (int k = 0; k < kChunkKeys; ++k) mask[k] = bits[k];
+    if (wave == 0) {
+        int nfree = 0, nmove = 0, all = 0;
+        for (int c = lane; c < chunks; c += 64) {
+            const int2 stays = a.chunk_stays[(long long)pair * a.chunks + c];
+            const int gone = max(0, min(kChunk, a.keep - c * kChunk)) - stays.x;
+            all += gone;
+            if (c < chunk) {
+                nfree += gone;
+                nmove += stays.y;
+            }
+        }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            nfree += __shfl_xor(nfree, o);
+            nmove += __shfl_xor(nmove, o);
+            all += __shfl_xor(all, o);
+        }
+        if (lane == 0) {
+            start[0] = nfree;
+            start[1] = nmove;
+            if (chunk == 0) a.count[pair] = all;
+        }
+    }
+    int nfree = 0, nmove = 0;
+#pragma unroll
+    for (int k = 0; k < kChunkKeys; ++k) {
+        const int i = chunk_row(chunk, k);
+        const bool stay = (mask[k] >> lane) & 1ull;
+        nfree += __popcll(__ballot(i < a.keep && !stay));
+        nmove += __popcll(__ballot(i >= a.keep && stay));
+    }
+    if (lane == 0) {
+        wave_free[wave] = nfree;
+        wave_move[wave] = nmove;
+    }
+    __syncthreads();
+    nfree = start[0], nmove = start[1];
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+        if (w < wave) {
+            nfree += wave_free[w];
+            nmove += wave_move[w];
+        }
+    int32_t *free_rows = a.moves + (long long)pair * 2 * a.most, *movers = free_rows + a.most;
+#pragma unroll
+    for (int k = 0; k < kChunkKeys; ++k) {
+        const int i = chunk_row(chunk, k);
+        const bool stay = (mask[k] >> lane) & 1ull, is_free = i < a.keep && !stay, moves = i >= a.keep && stay;
+        const unsigned long long fm = __ballot(is_free), mm = __ballot(moves);
+        if (is_free) free_rows[nfree + below(fm)] = i;
+        if (moves) movers[nmove + below(mm)] = i;
+        nfree += __popcll(fm);
+        nmove += __popcll(mm);
+        if (stay && !moves) leave_row(a, pair, i);
+    }
 }
 
 __global__ void __launch_bounds__(256)
@@ -149,23 +499,12 @@ evict_move(EvictArgs a)
 {
     const int pair = blockIdx.y + blockIdx.z * gridDim.y;
     if (pair >= a.S * a.H) return;
-    const int s = pair / a.H, h = pair % a.H;
-    if (blockIdx.x == 0 && h == 0 && threadIdx.x == 0) a.len_out[s] = min(paged_rows(a.len[s], a.per_seq * a.page), a.keep);
-    const int count = a.count[pair];
-    const int32_t *free_rows = a.moves + (long long)pair * 2 * a.most, *movers = free_rows + a.most;
-    const int32_t *table = a.table + (long long)s * a.per_seq;
-    const int pieces = a.row_bytes / 16;
-    for (long long i = blockIdx.x * 256 + threadIdx.x; i < (long long)count * 2 * pieces; i += (long long)gridDim.x * 256) {
-        const int j = (int)(i / (2 * pieces)), w = (int)(i % (2 * pieces));
-        const int to = free_rows[j], from = movers[j];
-        const int to_page = table[to / a.page];
-        if ((unsigned)to_page >= (unsigned)a.pages) continue;
-        char *pool = reinterpret_cast<char *>(w < pieces ? a.K : a.V);
-        const long long src = paged_base(table[from / a.page], a.pages, a.H, h, a.page) + from % a.page;
-        const long long dst = paged_base(to_page, a.pages, a.H, h, a.page) + to % a.page;
-        *reinterpret_cast<uint4 *>(pool + dst * a.row_bytes + (w % pieces) * 16) =
-            *reinterpret_cast<const uint4 *>(pool + src * a.row_bytes + (w % pieces) * 16);
-    }
+    // (nothing else here looks at the lengths: len_out may be where they came from)
+    if (blockIdx.x == 0 && pair % a.H == 0 && threadIdx.x == 0) a.len_out[pair / a.H] = min(a.rows_of(pair / a.H), a.keep);
+    const int32_t *free_rows = a.moves + (long long)pair * 2 * a.most;
+    const int pieces = a.row_bytes / 16, per = 256 / pieces;
+    move_rows<4>(a, pair, free_rows, free_rows + a.most, a.count[pair], blockIdx.x * per + threadIdx.x / pieces, gridDim.x * per,
+                 threadIdx.x % pieces);
 }
 
 }  // namespace
@@ -175,23 +514,54 @@ hipError_t launch_paged_evict(const ws_paged_cache &c, int keep, int sinks, int 
                               void *ws, hipStream_t st)
 {
     const int cap = c.per_seq * c.page, pairs = c.S * c.Hkv;
+    const PagedEvictSpace sp = paged_evict_space(c.S, c.Hkv, cap, keep);
+    char *base = reinterpret_cast<char *>(ws);
     EvictArgs a = {};
     a.K = c.K, a.V = c.V, a.table = c.table, a.len = c.len;
-    a.pages = c.pages, a.H = c.Hkv, a.page = c.page, a.S = c.S, a.per_seq = c.per_seq;
+    a.pages = c.pages, a.H = c.Hkv, a.page_shift = __builtin_ctz((unsigned)c.page), a.S = c.S, a.per_seq = c.per_seq;
     a.row_bytes = c.d * (c.dt == WS_BF16 ? 2 : 4);
     a.keep = keep, a.sinks = sinks, a.recent = recent;
     a.seen = seen, a.stamp_in = stamp_in, a.mass_in = mass_in;
     a.mass_out = mass_out, a.stamp_out = stamp_out, a.len_out = len_out, a.kept = kept;
-    a.most = paged_evict_moves(cap, keep);
-    a.count = reinterpret_cast<int32_t *>(ws);
-    a.moves = reinterpret_cast<int32_t *>(reinterpret_cast<char *>(ws) + round_up((size_t)pairs * sizeof(int32_t), 256));
-    hipLaunchKernelGGL(evict_pick, dim3((unsigned)pairs), dim3(kPick), 0, st, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const long long work = ((long long)a.most * 2 * (a.row_bytes / 16) + 255) / 256;
-    const long long share = 4096 / pairs > 1 ? 4096 / pairs : 1;
+    a.most = paged_evict_moves(cap, keep), a.chunks = paged_evict_chunks(cap);
+    a.count = reinterpret_cast<int32_t *>(base);
+    a.moves = reinterpret_cast<int32_t *>(base + sp.moves);
+    a.keys = reinterpret_cast<uint32_t *>(base + sp.keys);
+    a.hist = reinterpret_cast<uint16_t *>(base + sp.hist);
+    a.cells = reinterpret_cast<uint2 *>(base + sp.cells);
+    a.chunk_stays = reinterpret_cast<int2 *>(base + sp.stays);
+    a.bits = reinterpret_cast<unsigned long long *>(base + sp.bits);
     const int y = pairs < 32768 ? pairs : 32768, z = (pairs + y - 1) / y;
-    hipLaunchKernelGGL(evict_move, dim3((unsigned)(work < share ? work : share), (unsigned)y, (unsigned)z), dim3(256), 0, st, a);
+    if (cap <= kPickRows) {
+        const bool move = a.most <= kInlineMoves;
+        const dim3 grid((unsigned)pairs);
+        if (cap <= 2048) {
+            if (move) hipLaunchKernelGGL((evict_pick<256, 8, true>), grid, dim3(256), 0, st, a);
+            else hipLaunchKernelGGL((evict_pick<256, 8, false>), grid, dim3(256), 0, st, a);
+        } else {
+            if (move) hipLaunchKernelGGL((evict_pick<1024, 16, true>), grid, dim3(1024), 0, st, a);
+            else hipLaunchKernelGGL((evict_pick<1024, 16, false>), grid, dim3(1024), 0, st, a);
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        if (move) {
+            // where the new lengths replace the old ones they wait until every head has read them
+            if (len_out == c.len) hipLaunchKernelGGL(evict_lengths, dim3((unsigned)((c.S + 255) / 256)), dim3(256), 0, st, a);
+            return hipGetLastError();
+        }
+    } else {
+        const dim3 grid((unsigned)a.chunks, (unsigned)y, (unsigned)z), block(256);
+        hipLaunchKernelGGL((evict_digit<0>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((evict_digit<1>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((evict_digit<2>), grid, block, 0, st, a);
+        hipLaunchKernelGGL(evict_count, grid, block, 0, st, a);
+        hipLaunchKernelGGL(evict_place, grid, block, 0, st, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const int per = 256 / (a.row_bytes / 16) * 4;
+    const long long want = (a.most + per - 1) / per, share = 8192 / pairs > 1 ? 8192 / pairs : 1;
+    hipLaunchKernelGGL(evict_move, dim3((unsigned)(want < share ? want : share), (unsigned)y, (unsigned)z), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 

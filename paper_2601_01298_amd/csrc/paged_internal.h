@@ -67,11 +67,26 @@ static inline size_t paged_attend_workspace_bytes(bool bf16, int S, int Hkv, int
 
 // Per KV head of a sequence: how many rows move, and from where to where.
 static inline int paged_evict_moves(int cap, int keep) { return keep >= cap ? 1 : (keep < cap - keep ? keep : cap - keep); }
-static inline size_t paged_evict_workspace_bytes(int S, int Hkv, int cap, int keep)
+constexpr int kPickRows = 16384;            // rows of a head whose choice one workgroup makes
+constexpr int kChunk = 4096;                // rows per workgroup of longer ones
+static inline int paged_evict_chunks(int cap) { return cap <= kPickRows ? 0 : (cap + kChunk - 1) / kChunk; }
+struct PagedEvictSpace {
+    size_t moves, keys, hist, cells, stays, bits, bytes;     // offsets, total; the counts of moves lie at 0
+};
+static inline PagedEvictSpace paged_evict_space(int S, int Hkv, int cap, int keep)
 {
-    const size_t pairs = (size_t)S * Hkv;
-    return round_up(pairs * sizeof(int32_t), 256) + round_up(pairs * paged_evict_moves(cap, keep) * 2 * sizeof(int32_t), 256);
+    PagedEvictSpace p;
+    const size_t pairs = (size_t)S * Hkv, chunks = pairs * paged_evict_chunks(cap);
+    p.moves = round_up(pairs * sizeof(int32_t), 256);
+    p.keys = p.moves + round_up(pairs * paged_evict_moves(cap, keep) * 2 * sizeof(int32_t), 256);
+    p.hist = p.keys + (chunks ? round_up(pairs * cap * sizeof(uint32_t), 256) : 0);
+    p.cells = p.hist + chunks * 3 * 2048 * sizeof(uint16_t);
+    p.stays = p.cells + (chunks ? round_up(pairs * 3 * 8, 256) : 0);
+    p.bits = p.stays + round_up(chunks * 8, 256);
+    p.bytes = p.bits + chunks * (kChunk / 8);
+    return p;
 }
+static inline size_t paged_evict_workspace_bytes(int S, int Hkv, int cap, int keep) { return paged_evict_space(S, Hkv, cap, keep).bytes; }
 
 // turns per unit of position of every pair, and the axis it goes by
 struct RotaryTable {
