@@ -17,6 +17,8 @@
 
 namespace ws {
 
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+
 namespace {
 
 constexpr int kDigits[3] = {11, 11, 10};
@@ -87,10 +89,18 @@ __device__ __forceinline__ int find_digit(const uint32_t (&c)[PER], uint32_t &le
     for (int w = 0; w < THREADS / 64 - 1; ++w)
         if (w < tid >> 6) above += wave_sum[w];
     if (above < left && left <= above + mine) {
-        int i = PER - 1;
-        while (above + c[i] < left) above += c[i--];
-        found[0] = PER * (THREADS - 1 - tid) + i;
-        found[1] = left - above;
+        int digit = PER * (THREADS - 1 - tid);
+        uint32_t over = above;
+#pragma unroll
+        for (int i = PER - 1; i >= 0; --i) {
+            if (above < left && left <= above + c[i]) {
+                digit += i;
+                over = above;
+            }
+            above += c[i];
+        }
+        found[0] = (uint32_t)digit;
+        found[1] = left - over;
     }
     __syncthreads();
     left = found[1];
@@ -119,22 +129,22 @@ __device__ __forceinline__ void move_rows(const EvictArgs &a, int pair, const in
             to_page[u] = table[to[u] >> a.page_shift];
             from_page[u] = table[from[u] >> a.page_shift];
         }
-        uint4 k[U], v[U];
+        u32x4_t k[U], v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const long long src = (paged_base(from_page[u], a.pages, a.H, h, 1 << a.page_shift) + (from[u] & pmask)) * a.row_bytes + piece * 16;
-            k[u] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(a.K) + src);
-            v[u] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(a.V) + src);
+            k[u] = *reinterpret_cast<const u32x4_t *>(reinterpret_cast<const char *>(a.K) + src);
+            v[u] = *reinterpret_cast<const u32x4_t *>(reinterpret_cast<const char *>(a.V) + src);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (j0 + u * groups >= count) break;
-            if ((unsigned)to_page[u] < (unsigned)a.pages) {
+            const bool there = j0 + u * groups < count;
+            if (there && (unsigned)to_page[u] < (unsigned)a.pages) {
                 const long long dst = (paged_base(to_page[u], a.pages, a.H, h, 1 << a.page_shift) + (to[u] & pmask)) * a.row_bytes + piece * 16;
-                *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(a.K) + dst) = k[u];
-                *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(a.V) + dst) = v[u];
+                __builtin_nontemporal_store(k[u], reinterpret_cast<u32x4_t *>(reinterpret_cast<char *>(a.K) + dst));
+                __builtin_nontemporal_store(v[u], reinterpret_cast<u32x4_t *>(reinterpret_cast<char *>(a.V) + dst));
             }
-            if (piece == 0) {
+            if (there && piece == 0) {
                 a.mass_out[at + to[u]] = a.mass_in[at + from[u]];
                 a.stamp_out[at + to[u]] = a.stamp_in[at + from[u]];
                 if (a.kept != nullptr) a.kept[(long long)pair * a.keep + to[u]] = from[u];
@@ -144,14 +154,15 @@ __device__ __forceinline__ void move_rows(const EvictArgs &a, int pair, const in
 }
 
 // A row that stays where it is: its account and stamp where they are wanted elsewhere.
-__device__ __forceinline__ void leave_row(const EvictArgs &a, int pair, int i)
+__device__ __forceinline__ void leave_row(const EvictArgs &a, int pair, int i, float mass, int stamp)
 {
     const long long at = (long long)pair * a.cap() + i;
-    if (a.mass_out != a.mass_in) a.mass_out[at] = a.mass_in[at];
-    if (a.stamp_out != a.stamp_in) a.stamp_out[at] = a.stamp_in[at];
+    if (a.mass_out != a.mass_in) a.mass_out[at] = mass;
+    if (a.stamp_out != a.stamp_in) a.stamp_out[at] = stamp;
     if (a.kept != nullptr) a.kept[(long long)pair * a.keep + i] = i;
 }
 
+constexpr int kMoveRows = 4;                // rows a thread of evict_move has on their way at once
 constexpr int kInlineMoves = 128;           // moves of a head that evict_pick makes itself
 
 // Wave w has rows 64 KPT w and up, KPT runs of 64: the order of rows is the order of waves, runs and lanes.
@@ -160,7 +171,7 @@ __global__ void __launch_bounds__(THREADS)
 evict_pick(EvictArgs a)
 {
     constexpr int WAVES = THREADS / 64;
-    __shared__ uint32_t hist[3][kBins];
+    __shared__ __attribute__((aligned(16))) uint32_t hist[kBins];
     __shared__ uint32_t wave_sum[WAVES], found[2];
     __shared__ int wave_ties[WAVES], wave_free[WAVES], wave_move[WAVES];
     __shared__ int32_t lists[2][MOVE ? kInlineMoves : 1];
@@ -169,23 +180,23 @@ evict_pick(EvictArgs a)
     const int n = a.rows_of(s);
     if (MOVE && pair % a.H == 0 && tid == 0 && a.len_out != a.len) a.len_out[s] = min(n, a.keep);
     const int row0 = wave * 64 * KPT + lane;
-    if (n <= a.keep) {
-        if (!MOVE && tid == 0) a.count[pair] = 0;
-#pragma unroll 4
-        for (int k = 0; k < KPT; ++k)
-            if (row0 + k * 64 < n) leave_row(a, pair, row0 + k * 64);
-        return;
-    }
     const long long at = (long long)pair * a.cap(), fresh = (long long)a.seen[s] - a.recent;
     float mass[KPT];
     int stamp[KPT];
 #pragma unroll
     for (int k = 0; k < KPT; ++k) {
-        const int i = min(row0 + k * 64, n - 1);
+        const int i = max(0, min(row0 + k * 64, n - 1));
         mass[k] = a.mass_in[at + i];
         stamp[k] = a.stamp_in[at + i];
     }
-    for (int i = tid; i < 3 * kBins; i += THREADS) (&hist[0][0])[i] = 0;
+    if (n <= a.keep) {
+        if (!MOVE && tid == 0) a.count[pair] = 0;
+#pragma unroll
+        for (int k = 0; k < KPT; ++k)
+            if (row0 + k * 64 < n) leave_row(a, pair, row0 + k * 64, mass[k], stamp[k]);
+        return;
+    }
+    for (int i = tid; i < kBins; i += THREADS) hist[i] = 0;
     __syncthreads();
     uint32_t key[KPT];
 #pragma unroll
@@ -198,12 +209,15 @@ evict_pick(EvictArgs a)
         shift -= kDigits[digit];
 #pragma unroll
         for (int k = 0; k < KPT; ++k)
-            if (row0 + k * 64 < n && (key[k] & known) == prefix) atomicAdd(&hist[digit][(key[k] >> shift) & ((1 << kDigits[digit]) - 1)], 1u);
+            if (row0 + k * 64 < n && (key[k] & known) == prefix) atomicAdd(&hist[(key[k] >> shift) & ((1 << kDigits[digit]) - 1)], 1u);
         __syncthreads();
         constexpr int PER = kBins / THREADS;
         uint32_t c[PER];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) c[i] = hist[digit][PER * (THREADS - 1 - tid) + i];
+        for (int i = 0; i < PER; ++i) {
+            c[i] = hist[PER * (THREADS - 1 - tid) + i];
+            hist[PER * (THREADS - 1 - tid) + i] = 0;             // for the next digit, which waits for find_digit's barriers
+        }
         prefix |= (uint32_t)find_digit<THREADS, PER>(c, left, wave_sum, found) << shift;
     }
     // rows with a larger key stay, and of those with this one the first `left`
@@ -254,7 +268,7 @@ evict_pick(EvictArgs a)
         if (moves) movers[nmove + below(mm)] = i;
         nfree += __popcll(fm);
         nmove += __popcll(mm);
-        if (stay && !moves) leave_row(a, pair, i);
+        if (stay && !moves) leave_row(a, pair, i, mass[k], stamp[k]);
     }
     if constexpr (MOVE) {
         __syncthreads();
@@ -313,13 +327,16 @@ evict_digit(EvictArgs a)
     if (pair >= a.S * a.H) return;
     const int n = a.rows_of(pair / a.H), chunks = (n + kChunk - 1) / kChunk;
     if (chunk >= chunks) return;
+    const long long at = (long long)pair * a.cap();
     if (n <= a.keep) {
         if (DIGIT == 0)
-            for (int k = 0; k < kChunkKeys; ++k)
-                if (chunk_row(chunk, k) < n) leave_row(a, pair, chunk_row(chunk, k));
+#pragma unroll 8
+            for (int k = 0; k < kChunkKeys; ++k) {
+                const int i = chunk_row(chunk, k);
+                if (i < n) leave_row(a, pair, i, a.mass_in[at + i], a.stamp_in[at + i]);
+            }
         return;
     }
-    const long long at = (long long)pair * a.cap();
     uint32_t key[kChunkKeys];
     if constexpr (DIGIT == 0) {
         const long long fresh = (long long)a.seen[pair / a.H] - a.recent;
@@ -437,6 +454,17 @@ evict_place(EvictArgs a)
     unsigned long long mask[kChunkKeys];
 #pragma unroll
     for (int k = 0; k < kChunkKeys; ++k) mask[k] = bits[k];
+    float mass[kChunkKeys];
+    int stamp[kChunkKeys];
+    const bool elsewhere = a.mass_out != a.mass_in || a.stamp_out != a.stamp_in;
+    const long long at = (long long)pair * a.cap();
+    if (elsewhere && chunk * kChunk < a.keep)
+#pragma unroll
+        for (int k = 0; k < kChunkKeys; ++k) {
+            const int i = min(chunk_row(chunk, k), n - 1);
+            mass[k] = a.mass_in[at + i];
+            stamp[k] = a.stamp_in[at + i];
+        }
     if (wave == 0) {
         int nfree = 0, nmove = 0, all = 0;
         for (int c = lane; c < chunks; c += 64) {
@@ -490,7 +518,7 @@ evict_place(EvictArgs a)
         if (moves) movers[nmove + below(mm)] = i;
         nfree += __popcll(fm);
         nmove += __popcll(mm);
-        if (stay && !moves) leave_row(a, pair, i);
+        if (stay && !moves) leave_row(a, pair, i, mass[k], stamp[k]);
     }
 }
 
@@ -503,7 +531,7 @@ evict_move(EvictArgs a)
     if (blockIdx.x == 0 && pair % a.H == 0 && threadIdx.x == 0) a.len_out[pair / a.H] = min(a.rows_of(pair / a.H), a.keep);
     const int32_t *free_rows = a.moves + (long long)pair * 2 * a.most;
     const int pieces = a.row_bytes / 16, per = 256 / pieces;
-    move_rows<4>(a, pair, free_rows, free_rows + a.most, a.count[pair], blockIdx.x * per + threadIdx.x / pieces, gridDim.x * per,
+    move_rows<kMoveRows>(a, pair, free_rows, free_rows + a.most, a.count[pair], blockIdx.x * per + threadIdx.x / pieces, gridDim.x * per,
                  threadIdx.x % pieces);
 }
 
@@ -559,7 +587,7 @@ hipError_t launch_paged_evict(const ws_paged_cache &c, int keep, int sinks, int 
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const int per = 256 / (a.row_bytes / 16) * 4;
+    const int per = 256 / (a.row_bytes / 16) * kMoveRows;
     const long long want = (a.most + per - 1) / per, share = 8192 / pairs > 1 ? 8192 / pairs : 1;
     hipLaunchKernelGGL(evict_move, dim3((unsigned)(want < share ? want : share), (unsigned)y, (unsigned)z), dim3(256), 0, st, a);
     return hipGetLastError();
