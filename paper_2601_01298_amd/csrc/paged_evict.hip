@@ -13,6 +13,8 @@
 //                between workgroups.
 //   evict_move   copies the rows of K and V, accounts and stamps from and to where the lists say.
 // Bound: HBM (the moved rows); for short heads the chain of barriers of evict_pick.
+#include <type_traits>
+
 #include "paged_internal.h"
 
 namespace ws {
@@ -563,13 +565,15 @@ hipError_t launch_paged_evict(const ws_paged_cache &c, int keep, int sinks, int 
     if (cap <= kPickRows) {
         const bool move = a.most <= kInlineMoves;
         const dim3 grid((unsigned)pairs);
-        if (cap <= 2048) {
-            if (move) hipLaunchKernelGGL((evict_pick<256, 8, true>), grid, dim3(256), 0, st, a);
-            else hipLaunchKernelGGL((evict_pick<256, 8, false>), grid, dim3(256), 0, st, a);
-        } else {
-            if (move) hipLaunchKernelGGL((evict_pick<1024, 16, true>), grid, dim3(1024), 0, st, a);
-            else hipLaunchKernelGGL((evict_pick<1024, 16, false>), grid, dim3(1024), 0, st, a);
-        }
+        auto pick = [&](auto threads, auto keys) {
+            constexpr int T = decltype(threads)::value, N = decltype(keys)::value;
+            if (move) hipLaunchKernelGGL((evict_pick<T, N, true>), grid, dim3(T), 0, st, a);
+            else hipLaunchKernelGGL((evict_pick<T, N, false>), grid, dim3(T), 0, st, a);
+        };
+        using std::integral_constant;
+        if (cap <= 2048) pick(integral_constant<int, 256>(), integral_constant<int, 8>());
+        else if (cap <= 8192) pick(integral_constant<int, 1024>(), integral_constant<int, 8>());
+        else pick(integral_constant<int, 1024>(), integral_constant<int, 16>());
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         if (move) {
