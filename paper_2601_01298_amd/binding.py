@@ -449,6 +449,12 @@ def ws_synapse_inject(Kc: torch.Tensor, Vc: torch.Tensor, L: int, Knew: torch.Te
     return L + m
 
 
+# The raw handle of a device's current stream and the current device, without the objects around them: a decode step makes
+# several calls of a few microseconds each.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 class PagedCache:
     """Pools K, V [pages, Hkv, page, d], table [S, per_seq] int32 page numbers, len [S] int32 rows in use: what the calls
     below work on.  The tensors stay the caller's; make a new PagedCache when one of them is replaced."""
@@ -457,53 +463,53 @@ class PagedCache:
         _dev(K, "K")
         if K.dim() != 4:
             raise ValueError("K must be [pages, Hkv, page, d]")
-        _want(V, "V", K.shape, K.dtype)
         if table.dim() != 2:
             raise ValueError("table must be [S, per_seq]")
-        _want(table, "table", table.shape, torch.int32)
-        _want(len, "len", (table.shape[0],), torch.int32)
         self.K, self.V, self.table, self.len = K, V, table, len
+        self.device, self.dtype = K.device, K.dtype
         self.pages, self.Hkv, self.page, self.d = K.shape
         self.S, self.per_seq = table.shape
         self.rows = self.per_seq * self.page
-        self.device = K.device
-        for t, name in ((V, "V"), (table, "table"), (len, "len")):
-            self._here(t, name)
-        self._c = _PagedCache(K.data_ptr(), V.data_ptr(), table.data_ptr(), len.data_ptr(), _dtype_code(K), self.pages, self.Hkv,
-                              self.page, self.d, self.S, self.per_seq)
+        self._per_seq, self._per_row = (self.S,), (self.S, self.Hkv, self.rows)
+        self._c = _PagedCache(K.data_ptr(), self._ptr(V, "V", tuple(K.shape), K.dtype), self._ptr(table, "table", tuple(table.shape), torch.int32),
+                              self._ptr(len, "len", self._per_seq, torch.int32), _dtype_code(K), self.pages, self.Hkv, self.page, self.d,
+                              self.S, self.per_seq)
+        self._ref = ctypes.byref(self._c)
+        self._pairs = {}
 
-    def _here(self, t: torch.Tensor, name: str):
-        if t.device != self.device:
+    def _ptr(self, t, name: str, shape, dtype):
+        """The address of an argument of this shape and type on the cache's device; None for None."""
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.shape != shape or t.device != self.device or not t.is_contiguous():
+            _want(t, name, shape, dtype)
             raise ValueError(f"{name} must be on the cache's device, {self.device}, not on {t.device}")
-
-    def _want(self, t: torch.Tensor, name: str, shape, dtype) -> torch.Tensor:
-        _want(t, name, shape, dtype)
-        self._here(t, name)
-        return t
+        return t.data_ptr()
 
     def _rows(self, t: torch.Tensor, name: str, T: int, heads: int) -> _Rows:
         """Rows [T, heads, d] of any strides over whole rows."""
-        if not t.is_cuda:
-            raise ValueError(f"{name} must be a device tensor")
-        self._here(t, name)
-        if t.dtype != self.K.dtype:
-            raise TypeError(f"{name} must be {self.K.dtype}, got {t.dtype}")
-        if tuple(t.shape) != (T, heads, self.d):
-            raise ValueError(f"{name} must have shape {(T, heads, self.d)}, got {tuple(t.shape)}")
-        token, head, element = t.stride()
-        if element != 1:
+        if t.dtype is not self.dtype or t.device != self.device or t.shape != (T, heads, self.d) or t.stride(2) != 1:
+            if t.dtype is not self.dtype:
+                raise TypeError(f"{name} must be {self.dtype}, got {t.dtype}")
+            if t.device != self.device:
+                raise ValueError(f"{name} must be on the cache's device, {self.device}, not on {t.device}")
+            if t.shape != (T, heads, self.d):
+                raise ValueError(f"{name} must have shape {(T, heads, self.d)}, got {tuple(t.shape)}")
             raise ValueError(f"the elements of a row of {name} must be contiguous")
-        return _Rows(t.data_ptr(), token, head)
+        return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+    def _workspace(self, t, op: str, stream, **kw):
+        if t is None:
+            return ws_synapse_paged_workspace(self, op, stream=stream, **kw)
+        if t.device != self.device or not t.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the cache's device")
+        return t
 
     def _stream(self, stream) -> int:
         """The stream to enqueue on; kernels are launched on the current device, so the cache has to be there."""
-        if self.device.index != torch.cuda.current_device():
+        if self.device.index != _device():
             raise ValueError(f"the cache is on {self.device}, the current device is {torch.cuda.current_device()}")
-        return _stream(stream)
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+        return _raw_stream(self.device.index) if stream is None else _stream(stream)
 
 
 def ws_synapse_paged_workspace(cache: PagedCache, op: str, Hq: int = 0, weights: bool = False, keep: int = 0, stream=None) -> torch.Tensor:
@@ -527,35 +533,31 @@ def ws_synapse_paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor,
     stamp [S,Hkv,rows] int32 (with seen [S] int32) and mass [S,Hkv,rows] fp32 are started for the new rows."""
     T = k.shape[0]
     krows, vrows = cache._rows(k, "k", T, cache.Hkv), cache._rows(v, "v", T, cache.Hkv)
-    cache._want(first, "first", (cache.S + 1,), torch.int32)
-    axes, npairs = 0, None
+    axes, npairs, posp = 0, None, None
     if pos is not None:
         axes = 1 if pos.dim() == 1 else pos.shape[0]
-        cache._want(pos, "pos", (T,) if pos.dim() == 1 else (axes, T), torch.int32)
-        pairs = [cache.d // 2] if pairs is None and axes == 1 else list(pairs or ())
-        if len(pairs) != axes:
-            raise ValueError("one number of pairs per axis")
-        npairs = (ctypes.c_int * axes)(*[int(n) for n in pairs])
-    qrows, Hq = None, 0
+        posp = cache._ptr(pos, "pos", (T,) if pos.dim() == 1 else (axes, T), torch.int32)
+        pairs = tuple(pairs) if pairs is not None else (cache.d // 2,) if axes == 1 else ()
+        npairs = cache._pairs.get(pairs)
+        if npairs is None or len(pairs) != axes:
+            if len(pairs) != axes:
+                raise ValueError("one number of pairs per axis")
+            npairs = cache._pairs[pairs] = (ctypes.c_int * axes)(*[int(n) for n in pairs])
+    qrows, Hq, qp = None, 0, None
     if q is not None:
         if q.dim() != 3:
             raise ValueError("q must be [T,Hq,d]")
         Hq = q.shape[1]
-        qrows = cache._rows(q, "q", T, Hq)
+        qrows = ctypes.byref(cache._rows(q, "q", T, Hq))
         if q_out is None:
             q_out = _new((T, Hq, cache.d), q.dtype, cache.device, stream)
-        cache._want(q_out, "q_out", (T, Hq, cache.d), q.dtype)
-    shape = (cache.S, cache.Hkv, cache.rows)
-    if seen is not None:
-        cache._want(seen, "seen", (cache.S,), torch.int32)
-    if stamp is not None:
-        cache._want(stamp, "stamp", shape, torch.int32)
-    if mass is not None:
-        cache._want(mass, "mass", shape, torch.float32)
-    _check(lib().ws_synapse_paged_append(ctypes.byref(cache._c), ctypes.byref(krows), ctypes.byref(vrows), T, first.data_ptr(), _ptr(pos),
-                                         axes, npairs, float(base), None if qrows is None else ctypes.byref(qrows), Hq,
-                                         _ptr(q_out) if q is not None else None, _ptr(seen), _ptr(stamp), _ptr(mass),
-                                         cache._stream(stream)), "ws_synapse_paged_append")
+        qp = cache._ptr(q_out, "q_out", (T, Hq, cache.d), cache.dtype)
+    _check(lib().ws_synapse_paged_append(cache._ref, ctypes.byref(krows), ctypes.byref(vrows), T,
+                                         cache._ptr(first, "first", (cache.S + 1,), torch.int32), posp, axes, npairs, base, qrows, Hq, qp,
+                                         cache._ptr(seen, "seen", cache._per_seq, torch.int32),
+                                         cache._ptr(stamp, "stamp", cache._per_row, torch.int32),
+                                         cache._ptr(mass, "mass", cache._per_row, torch.float32), cache._stream(stream)),
+           "ws_synapse_paged_append")
     return q_out
 
 
@@ -567,25 +569,15 @@ def ws_synapse_paged_attend(cache: PagedCache, Q: torch.Tensor, scale: float = 0
     if Q.dim() != 3:
         raise ValueError("Q must be [S,Hq,d]")
     Hq = Q.shape[1]
-    cache._want(Q, "Q", (cache.S, Hq, cache.d), cache.K.dtype)
+    shape = (cache.S, Hq, cache.d)
     if O is None:
-        O = _new((cache.S, Hq, cache.d), torch.float32, cache.device, stream)
-    cache._want(O, "O", (cache.S, Hq, cache.d), torch.float32)
-    if lse is not None:
-        cache._want(lse, "lse", (cache.S, Hq), torch.float32)
-    shape = (cache.S, cache.Hkv, cache.rows)
-    if mass_in is not None:
-        cache._want(mass_in, "mass_in", shape, torch.float32)
-    if mass_out is not None:
-        cache._want(mass_out, "mass_out", shape, torch.float32)
-    if workspace is None:
-        workspace = ws_synapse_paged_workspace(cache, "attend", Hq, mass_out is not None, stream=stream)
-    else:
-        workspace = _workspace(0, cache.device, workspace)
-        cache._here(workspace, "workspace")
-    _check(lib().ws_synapse_paged_attend(ctypes.byref(cache._c), Q.data_ptr(), Hq, float(scale), O.data_ptr(), _ptr(lse), float(decay),
-                                         _ptr(mass_in), _ptr(mass_out), workspace.data_ptr(), workspace.nbytes,
-                                         cache._stream(stream)), "ws_synapse_paged_attend")
+        O = _new(shape, torch.float32, cache.device, stream)
+    qp, op = cache._ptr(Q, "Q", shape, cache.dtype), cache._ptr(O, "O", shape, torch.float32)
+    workspace = cache._workspace(workspace, "attend", stream, Hq=Hq, weights=mass_out is not None)
+    _check(lib().ws_synapse_paged_attend(cache._ref, qp, Hq, scale, op, cache._ptr(lse, "lse", (cache.S, Hq), torch.float32), decay,
+                                         cache._ptr(mass_in, "mass_in", cache._per_row, torch.float32),
+                                         cache._ptr(mass_out, "mass_out", cache._per_row, torch.float32), workspace.data_ptr(),
+                                         workspace.nbytes, cache._stream(stream)), "ws_synapse_paged_attend")
     return O
 
 
@@ -594,21 +586,15 @@ def ws_synapse_paged_evict(cache: PagedCache, keep: int, seen: torch.Tensor, mas
                            len_out: torch.Tensor | None = None, kept: torch.Tensor | None = None, workspace=None, stream=None):
     """Every sequence is cut to `keep` rows per KV head: the protected ones and those with the largest mass.  K and V move in
     place; mass, stamp [S,Hkv,rows] and len [S] too, unless mass_out, stamp_out, len_out are given.  Returns len_out."""
-    shape = (cache.S, cache.Hkv, cache.rows)
-    cache._want(seen, "seen", (cache.S,), torch.int32)
-    cache._want(mass_in, "mass_in", shape, torch.float32)
-    cache._want(stamp_in, "stamp_in", shape, torch.int32)
-    mass_out = mass_in if mass_out is None else cache._want(mass_out, "mass_out", shape, torch.float32)
-    stamp_out = stamp_in if stamp_out is None else cache._want(stamp_out, "stamp_out", shape, torch.int32)
-    len_out = cache.len if len_out is None else cache._want(len_out, "len_out", (cache.S,), torch.int32)
-    if kept is not None:
-        cache._want(kept, "kept", (cache.S, cache.Hkv, keep), torch.int32)
-    if workspace is None:
-        workspace = ws_synapse_paged_workspace(cache, "evict", keep=keep, stream=stream)
-    else:
-        workspace = _workspace(0, cache.device, workspace)
-        cache._here(workspace, "workspace")
-    _check(lib().ws_synapse_paged_evict(ctypes.byref(cache._c), int(keep), int(sinks), int(recent), seen.data_ptr(), mass_in.data_ptr(),
-                                        mass_out.data_ptr(), stamp_in.data_ptr(), stamp_out.data_ptr(), len_out.data_ptr(), _ptr(kept),
-                                        workspace.data_ptr(), workspace.nbytes, cache._stream(stream)), "ws_synapse_paged_evict")
+    mass_out = mass_in if mass_out is None else mass_out
+    stamp_out = stamp_in if stamp_out is None else stamp_out
+    len_out = cache.len if len_out is None else len_out
+    workspace = cache._workspace(workspace, "evict", stream, keep=keep)
+    ptr, per_row = cache._ptr, cache._per_row
+    _check(lib().ws_synapse_paged_evict(cache._ref, keep, sinks, recent, ptr(seen, "seen", cache._per_seq, torch.int32),
+                                        ptr(mass_in, "mass_in", per_row, torch.float32), ptr(mass_out, "mass_out", per_row, torch.float32),
+                                        ptr(stamp_in, "stamp_in", per_row, torch.int32), ptr(stamp_out, "stamp_out", per_row, torch.int32),
+                                        ptr(len_out, "len_out", cache._per_seq, torch.int32),
+                                        ptr(kept, "kept", (cache.S, cache.Hkv, keep), torch.int32), workspace.data_ptr(), workspace.nbytes,
+                                        cache._stream(stream)), "ws_synapse_paged_evict")
     return len_out

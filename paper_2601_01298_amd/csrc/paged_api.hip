@@ -59,12 +59,16 @@ ws_status ws_synapse_paged_append(const ws_paged_cache *cache, const ws_rows *k,
     if (pos) {
         if (!pairs_host || !(base > 0.0f) || !std::isfinite(base)) return WS_ERR_INVALID_ARG;
         if (axes < 1 || axes > ws::kMaxAxes) return WS_ERR_UNSUPPORTED;
+        // base^(-2c/d) turns / (2 pi) pair by pair; 64 products in 64 bits of mantissa are off by less than half a step of the result
+        const long double step = std::pow((long double)base, -2.0L / cache->d);
+        long double turns = 1.0L / 6.283185307179586476925286766559L;
         int c = 0;
         for (int a = 0; a < axes; ++a) {
             if (pairs_host[a] < 0 || pairs_host[a] > half - c) return WS_ERR_INVALID_ARG;
             for (int i = 0; i < pairs_host[a]; ++i, ++c) {
                 rot.axis[c] = (unsigned char)a;
-                rot.turns[c] = std::pow((double)base, -2.0 * c / cache->d) / 6.283185307179586476925;
+                rot.turns[c] = (double)turns;
+                turns *= step;
             }
         }
         if (c != half) return WS_ERR_INVALID_ARG;
