@@ -466,7 +466,7 @@ class PagedCache:
         if table.dim() != 2:
             raise ValueError("table must be [S, per_seq]")
         self.K, self.V, self.table, self.len = K, V, table, len
-        self.device, self.dtype = K.device, K.dtype
+        self.device, self.dtype, self._index = K.device, K.dtype, K.get_device()
         self.pages, self.Hkv, self.page, self.d = K.shape
         self.S, self.per_seq = table.shape
         self.rows = self.per_seq * self.page
@@ -481,35 +481,36 @@ class PagedCache:
         """The address of an argument of this shape and type on the cache's device; None for None."""
         if t is None:
             return None
-        if t.dtype is not dtype or t.shape != shape or t.device != self.device or not t.is_contiguous():
-            _want(t, name, shape, dtype)
-            raise ValueError(f"{name} must be on the cache's device, {self.device}, not on {t.device}")
-        return t.data_ptr()
+        if t.get_device() == self._index and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+            return t.data_ptr()
+        _want(t, name, shape, dtype)
+        raise ValueError(f"{name} must be on the cache's device, {self.device}, not on {t.device}")
 
     def _rows(self, t: torch.Tensor, name: str, T: int, heads: int) -> _Rows:
         """Rows [T, heads, d] of any strides over whole rows."""
-        if t.dtype is not self.dtype or t.device != self.device or t.shape != (T, heads, self.d) or t.stride(2) != 1:
-            if t.dtype is not self.dtype:
-                raise TypeError(f"{name} must be {self.dtype}, got {t.dtype}")
-            if t.device != self.device:
-                raise ValueError(f"{name} must be on the cache's device, {self.device}, not on {t.device}")
-            if t.shape != (T, heads, self.d):
-                raise ValueError(f"{name} must have shape {(T, heads, self.d)}, got {tuple(t.shape)}")
-            raise ValueError(f"the elements of a row of {name} must be contiguous")
-        return _Rows(t.data_ptr(), t.stride(0), t.stride(1))
+        stride = t.stride()
+        if t.get_device() == self._index and t.dtype is self.dtype and t.shape == (T, heads, self.d) and stride[2] == 1:
+            return _Rows(t.data_ptr(), stride[0], stride[1])
+        if t.dtype is not self.dtype:
+            raise TypeError(f"{name} must be {self.dtype}, got {t.dtype}")
+        if t.device != self.device:
+            raise ValueError(f"{name} must be on the cache's device, {self.device}, not on {t.device}")
+        if t.shape != (T, heads, self.d):
+            raise ValueError(f"{name} must have shape {(T, heads, self.d)}, got {tuple(t.shape)}")
+        raise ValueError(f"the elements of a row of {name} must be contiguous")
 
     def _workspace(self, t, op: str, stream, **kw):
         if t is None:
             return ws_synapse_paged_workspace(self, op, stream=stream, **kw)
-        if t.device != self.device or not t.is_contiguous():
+        if t.get_device() != self._index or not t.is_contiguous():
             raise ValueError("workspace must be a contiguous tensor on the cache's device")
         return t
 
     def _stream(self, stream) -> int:
         """The stream to enqueue on; kernels are launched on the current device, so the cache has to be there."""
-        if self.device.index != _device():
+        if self._index != _device():
             raise ValueError(f"the cache is on {self.device}, the current device is {torch.cuda.current_device()}")
-        return _raw_stream(self.device.index) if stream is None else _stream(stream)
+        return _raw_stream(self._index) if stream is None else _stream(stream)
 
 
 def ws_synapse_paged_workspace(cache: PagedCache, op: str, Hq: int = 0, weights: bool = False, keep: int = 0, stream=None) -> torch.Tensor:
