@@ -106,56 +106,61 @@ struct Merge {
     }
 };
 
-// Tiles [ta, tb) of sequence s's head h (n rows) for query heads q0 .. of it; the waves' parts are left in `red`, behind a barrier.
+// One wave's way through tiles of a (sequence, KV head, query heads).  begin() says which and asks for the first tile, run() goes through
+// them, leave() puts the wave's part into LDS; begin() of the next ones may come before leave(), so that their first tile is on its
+// way while the waves' parts are put together.
 template <bool BF16, int D, int SINK>
-__device__ __forceinline__ void sweep(const AttendArgs &a, int s, int h, int q0, int n, int ta, int tb, Merge<D> &red, float *kept,
-                                      int kept_stride)
-{
+struct Sweep {
     using P = Shape<BF16, D>;
-    constexpr int TR = P::TR, RB = P::RB, HV = P::HV, NK = P::NK, C = P::C, VW = P::VW, NV = P::NV;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int lq = lane & 15, lj = lane >> 4;
-    const int cap = a.per_seq << a.page_shift, pmask = (1 << a.page_shift) - 1;
-    const int g = a.Hq / a.H, gt = min(kPagedQueries, g - q0);
-    const long long qrow = (long long)s * a.Hq + h * g + q0;
+    static constexpr int TR = P::TR, RB = P::RB, HV = P::HV, NK = P::NK, C = P::C, VW = P::VW, NV = P::NV;
+    const AttendArgs &a;
+    const int lane, wave, lq, lj, pmask, g;
+    const unsigned koff, voff;
+    float *const kept;                                   // kToLds: [g][kept_stride]
+    const int kept_stride;
+    // which tiles
+    int s, h, q0, n, t, tb, gt, last16;
+    scalar_i32 table;
     __amdgpu_buffer_rsrc_t logits;
-    if constexpr (SINK == kToMemory) {
-        // the logits of this head's query heads, from the first one of this tile of them on
-        float *p = a.logits + ((long long)(s * a.H + h) * logit_rows(cap) * g + q0 * 16);
-        logits = __builtin_amdgcn_make_buffer_rsrc(p, 0, (logit_rows(cap) * g - q0 * 16) * 4, 0x00020000);
-    }
-    const scalar_i32 table = as_scalar(a.table) + (long long)s * a.per_seq;
-    const int last16 = (n - 1) & ~15;                // a tile's second half may not exist: it reads this one instead
-
-    // queries: the lane's part of query lq's row, in the order of the K loads; heads that do not exist are zero
+    // the tile on its way, the pages of the next one, the queries
+    Tile<BF16, D> x;
+    int id[HV];
     uint4 qf[NK];
-#pragma unroll
-    for (int kk = 0; kk < NK; ++kk) {
-        qf[kk] = make_uint4(0, 0, 0, 0);
-        if (lq < gt)
-            qf[kk] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(a.Q) + (qrow + lq) * RB + kk * 64 + lj * 16);
+    // what is there: maximum and sum (of the lane's rows) of query lq, output
+    float m, l;
+    f32x4_t acc[C];
+
+    __device__ __forceinline__ Sweep(const AttendArgs &args, float *k, int stride)
+        : a(args), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lq(lane & 15), lj(lane >> 4),
+          pmask((1 << args.page_shift) - 1), g(args.Hq / args.H), koff(lq * RB + lj * 16), voff(4 * lj * RB + lq * VW * 4), kept(k),
+          kept_stride(stride)
+    {
     }
-    auto pages_of = [&](int t, int (&id)[HV]) {
+
+    __device__ __forceinline__ void pages_of(int tile, int (&to)[HV]) const
+    {
 #pragma unroll
-        for (int hf = 0; hf < HV; ++hf) id[hf] = table[min(t * TR + 16 * hf, last16) >> a.page_shift];
-    };
-    auto half_base = [&](int t, int hf, int id) {    // where half hf of tile t starts in the pools
-        const int r = min(t * TR + 16 * hf, last16);
-        return (unsigned long long)(paged_base(id, a.pages, a.H, h, 1 << a.page_shift) + (r & pmask)) * RB;
-    };
-    const unsigned koff = lq * RB + lj * 16, voff = 4 * lj * RB + lq * VW * 4;
-    auto load_k = [&](Tile<BF16, D> &x, int t, const int (&id)[HV]) {
+        for (int hf = 0; hf < HV; ++hf) to[hf] = table[min(tile * TR + 16 * hf, last16) >> a.page_shift];
+    }
+    __device__ __forceinline__ unsigned long long half_base(int tile, int hf, int page) const    // where a half starts in the pools
+    {
+        const int r = min(tile * TR + 16 * hf, last16);
+        return (unsigned long long)(paged_base(page, a.pages, a.H, h, 1 << a.page_shift) + (r & pmask)) * RB;
+    }
+    __device__ __forceinline__ void load_k(int tile)
+    {
 #pragma unroll
         for (int hf = 0; hf < HV; ++hf) {
-            const char *p = reinterpret_cast<const char *>(a.K) + half_base(t, hf, id[hf]);
+            const char *p = reinterpret_cast<const char *>(a.K) + half_base(tile, hf, id[hf]);
 #pragma unroll
             for (int kk = 0; kk < NK; ++kk) x.k[hf][kk] = load16(p + koff + kk * 64);
         }
-    };
-    auto load_v = [&](Tile<BF16, D> &x, int t, const int (&id)[HV]) {
+    }
+    __device__ __forceinline__ void load_v(int tile)
+    {
 #pragma unroll
         for (int hf = 0; hf < HV; ++hf) {
-            const char *p = reinterpret_cast<const char *>(a.V) + half_base(t, hf, id[hf]);
+            const char *p = reinterpret_cast<const char *>(a.V) + half_base(tile, hf, id[hf]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if constexpr (VW == 2) {
@@ -172,19 +177,40 @@ __device__ __forceinline__ void sweep(const AttendArgs &a, int s, int h, int q0,
                 }
             }
         }
-    };
+    }
 
-    float m = -__builtin_inff(), l = 0.0f;           // of query lq; l of the lane's rows only
-    f32x4_t acc[C];
+    // Tiles [ta, to) of sequence s_'s head h_ (n_ > 0 rows), for its query heads q0_ ..
+    __device__ __forceinline__ void begin(int s_, int h_, int q0_, int n_, int ta, int to)
+    {
+        s = s_, h = h_, q0 = q0_, n = n_, t = ta + wave, tb = to;
+        gt = min(kPagedQueries, g - q0);
+        last16 = (n - 1) & ~15;                          // a tile's second half may not exist: it reads this one instead
+        table = as_scalar(a.table) + (long long)s * a.per_seq;
+        if constexpr (SINK == kToMemory) {
+            // the logits of this head's query heads, from the first one of this tile of them on
+            const int rows = logit_rows(a.per_seq << a.page_shift);
+            float *p = a.logits + ((long long)(s * a.H + h) * rows * g + q0 * 16);
+            logits = __builtin_amdgcn_make_buffer_rsrc(p, 0, (rows * g - q0 * 16) * 4, 0x00020000);
+        }
+        if (t >= tb) return;
+        pages_of(t, id);
+        load_k(t);
+        // the lane's part of query lq's row, in the order of the K loads; heads that do not exist are zero
+        const char *q = reinterpret_cast<const char *>(a.Q) + ((long long)s * a.Hq + h * g + q0 + lq) * RB + lj * 16;
 #pragma unroll
-    for (int c = 0; c < C; ++c) acc[c] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int kk = 0; kk < NK; ++kk) {
+            qf[kk] = make_uint4(0, 0, 0, 0);
+            if (lq < gt) qf[kk] = *reinterpret_cast<const uint4 *>(q + kk * 64);
+        }
+        load_v(t);
+        pages_of(t + 4, id);
+    }
 
-    Tile<BF16, D> x;
-    int id[HV];                                      // pages of the tile to load next
-    // One tile, held in x.  MORE: the wave's next tile, t + 4, is loaded behind the last use of K and of V (so one of the two
-    // is always on its way), and the pages of the one after it are looked up; a tile with another one behind it is whole.
-    auto tile = [&](int t, auto more) {
-        constexpr bool MORE = decltype(more)::value;
+    // One tile, held in x.  MORE: the wave's next tile, t + 4, is loaded behind the last use of K and of V (so one of the two is always
+    // on its way), and the pages of the one after it are looked up; a tile with another one behind it is whole.
+    template <bool MORE>
+    __device__ __forceinline__ void tile()
+    {
         int id2[HV];
         if constexpr (MORE) pages_of(t + 8, id2);
         // scores of rows 16 hf + 4 lj + i for query lq
@@ -206,7 +232,7 @@ __device__ __forceinline__ void sweep(const AttendArgs &a, int s, int h, int q0,
                 }
             }
         }
-        if constexpr (MORE) load_k(x, t + 4, id);
+        if constexpr (MORE) load_k(t + 4);
         const int r0 = t * TR + 4 * lj;              // the lane's first row
         float top = -__builtin_inff();
 #pragma unroll
@@ -298,25 +324,28 @@ __device__ __forceinline__ void sweep(const AttendArgs &a, int s, int h, int q0,
                     acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[i][c]), p[0][i], acc[c], 0, 0, 0);
         }
         if constexpr (MORE) {
-            load_v(x, t + 4, id);
+            load_v(t + 4);
 #pragma unroll
             for (int hf = 0; hf < HV; ++hf) id[hf] = id2[hf];
         }
-    };
-    int t = ta + wave;
-    if (t < tb) {
-        pages_of(t, id);
-        load_k(x, t, id);
-        load_v(x, t, id);
-        pages_of(t + 4, id);
-        for (; t + 4 < tb; t += 4) tile(t, std::true_type());
-        tile(t, std::false_type());
     }
 
-    // ---- the four waves' parts, through LDS: lane (lq, lj) holds head dimensions 4 C lj .. 4 C (lj + 1) - 1 of query lq
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (lq < gt) {
+    __device__ __forceinline__ void run()
+    {
+        m = -__builtin_inff(), l = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) acc[c] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        if (t >= tb) return;
+        for (; t + 4 < tb; t += 4) tile<true>();
+        tile<false>();
+    }
+
+    // Lane (lq, lj) holds head dimensions 4 C lj .. 4 C (lj + 1) - 1 of query lq, of `queries` there are.
+    __device__ __forceinline__ void leave(Merge<D> &red, int queries)
+    {
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (lq >= queries) return;
         if (lj == 0) {
             red.m[wave][lq] = m;
             red.l[wave][lq] = l;
@@ -328,8 +357,7 @@ __device__ __forceinline__ void sweep(const AttendArgs &a, int s, int h, int q0,
                 *reinterpret_cast<f32x4_t *>(&red.part[wave][lq][(4 * lj + i) * C + c]) =
                     f32x4_t{acc[c][i], acc[c + 1][i], acc[c + 2][i], acc[c + 3][i]};
     }
-    __syncthreads();
-}
+};
 
 template <bool BF16, int D, bool WEIGHTS>
 __global__ void __launch_bounds__(256, 3)
@@ -376,24 +404,36 @@ paged_split(AttendArgs a)
             ++s;
         }
     }
+    // ---- its parts of pairs, one after the other; a part's first tile is asked for before the one before it is put together
     const int run0 = t0;
-    while (t0 < t1) {
-        const int n = paged_rows(as_scalar(a.len)[s], cap);
-        const int ts = (n + TR - 1) / TR;                // tiles of a pair of this sequence
-        if (ts == 0 || t0 >= first + ts * pairs) {
+    Sweep<BF16, D, WEIGHTS ? kToMemory : kNowhere> w(a, nullptr, 0);
+    int pair, pair0, ts;                                 // the part at t0: its pair within the sequence, the pair's first tile, its tiles
+    auto begin = [&]() {
+        int n;
+        for (;;) {
+            n = paged_rows(as_scalar(a.len)[s], cap);
+            ts = (n + TR - 1) / TR;
+            if (ts != 0 && t0 < first + ts * pairs) break;
             first += ts * pairs;
             ++s;
-            continue;
         }
-        const int pair = (t0 - first) / ts;              // head and query tile
-        const int pair0 = first + pair * ts;
-        const int ta = t0 - pair0, tb = min(ts, t1 - pair0);
-        const int h = pair / a.tiles_q, q0 = pair % a.tiles_q * kPagedQueries;
-        const int gt = min(kPagedQueries, g - q0);
-        const long long qrow = (long long)s * a.Hq + h * g + q0;
-        sweep<BF16, D, WEIGHTS ? kToMemory : kNowhere>(a, s, h, q0, n, ta, tb, red, nullptr, 0);
-        const bool all = ta == 0 && tb == ts;            // nobody else has a part of this pair
+        pair = (t0 - first) / ts;
+        pair0 = first + pair * ts;
+        w.begin(s, pair / a.tiles_q, pair % a.tiles_q * kPagedQueries, n, t0 - pair0, min(ts, t1 - pair0));
+    };
+    begin();
+    for (;;) {
+        w.run();
+        const long long qrow = (long long)s * a.Hq + w.h * g + w.q0;
+        const int gt = w.gt, end = min(pair0 + ts, t1);
+        const bool all = t0 == pair0 && end == pair0 + ts;       // nobody else has a part of this pair
         const int slot = 2 * b + (t0 == run0 ? 0 : 1);
+        if (t0 == pair0 && tid == 0) a.start[(long long)s * pairs + pair] = pair0;
+        t0 = end;
+        const bool more = t0 < t1;
+        if (more) begin();
+        w.leave(red, gt);
+        __syncthreads();
         for (int i = tid; i < gt * D; i += 256) {
             const int q = i / D, e = i % D;
             float top, lsum, sum;
@@ -414,9 +454,8 @@ paged_split(AttendArgs a)
                 }
             }
         }
-        if (ta == 0 && tid == 0) a.start[(long long)s * pairs + pair] = pair0;
+        if (!more) return;
         __syncthreads();
-        t0 = pair0 + tb;
     }
 }
 
@@ -460,7 +499,11 @@ paged_whole(AttendArgs a, int kept_stride)
         if (tid < gt && a.lse != nullptr) a.lse[qrow + tid] = -__builtin_inff();
         return;
     }
-    sweep<BF16, D, WEIGHTS ? kToLds : kNowhere>(a, s, h, q0, n, 0, (n + TR - 1) / TR, red, kept, kept_stride);
+    Sweep<BF16, D, WEIGHTS ? kToLds : kNowhere> w(a, kept, kept_stride);
+    w.begin(s, h, q0, n, 0, (n + TR - 1) / TR);
+    w.run();
+    w.leave(red, gt);
+    __syncthreads();
     for (int i = tid; i < gt * D; i += 256) {
         const int q = i / D, e = i % D;
         float top, lsum, sum;
@@ -631,7 +674,7 @@ hipError_t launch_paged_attend(const ws_paged_cache &c, const void *Q, int Hq, f
     a.logits = mass_out ? reinterpret_cast<float *>(base + sp.logits) : nullptr;
     a.O = O, a.lse = lse, a.mass_in = mass_in, a.mass_out = mass_out, a.decay = decay;
     a.aligned = ((reinterpret_cast<uintptr_t>(mass_in) | reinterpret_cast<uintptr_t>(mass_out)) & 15) == 0;
-    const int groups = paged_groups(bf16, c.S, c.Hkv, Hq, cap);
+    const int groups = paged_groups(bf16, c.S, c.Hkv, Hq, cap, c.d);
     auto go = [&](auto BF, auto DD) {
         constexpr bool B = decltype(BF)::value;
         constexpr int D = decltype(DD)::value;

@@ -9,7 +9,7 @@ constexpr int kMaxAxes = 4;
 
 // How a launch of the attention is shared out.  The rows of all (sequence, KV head, up to 16 of its query heads) are counted off in
 // tiles, and every workgroup takes an equal run of tiles, across the borders of heads and sequences.
-constexpr int kPagedGroups = 768;           // workgroups of a full launch: three per compute unit
+constexpr int kPagedGroups = 512;           // most workgroups of a launch
 constexpr int kPagedQueries = 16;           // query heads a workgroup serves from one reading of the rows: the matrix tile's width
 static inline int paged_tile_rows(bool bf16) { return bf16 ? 32 : 16; }
 static inline int paged_query_tiles(int g) { return (g + kPagedQueries - 1) / kPagedQueries; }
@@ -19,10 +19,15 @@ static inline long long paged_most_tiles(bool bf16, int S, int Hkv, int Hq, int 
     const int tr = paged_tile_rows(bf16);
     return (long long)S * Hkv * paged_query_tiles(Hq / Hkv) * ((cap + tr - 1) / tr);
 }
-static inline int paged_groups(bool bf16, int S, int Hkv, int Hq, int cap)
+// One workgroup of four waves per compute unit keeps the memory busiest (8 heads of 131072 rows, d = 128: 84 us with 256, 88 with 512, 90
+// with 768; 256 heads of 32768 rows, d = 64: 309, 325, 328).  Where a tile is only 4 KB and a workgroup has few of them, two hide more of
+// the way from one head to the next (128 heads of up to 4000 rows, bf16, d = 64: 21.5 us with 256, 18.7 with 512; 72 heads of up to 4100,
+// fp32, d = 64: 17.6, 16.3; but 64 heads of 2048, d = 128: 19.4, 20.2).
+static inline int paged_groups(bool bf16, int S, int Hkv, int Hq, int cap, int d)
 {
-    const long long want = (paged_most_tiles(bf16, S, Hkv, Hq, cap) + 3) / 4;        // four waves, a tile each
-    return (int)(want < kPagedGroups ? want : kPagedGroups);
+    const long long tiles = paged_most_tiles(bf16, S, Hkv, Hq, cap), want = (tiles + 3) / 4;     // four waves, a tile each
+    const int most = d == 128 || tiles >= 256 * 256 ? 256 : kPagedGroups;
+    return (int)(want < most ? want : most);
 }
 
 // whole tiles of logits per query head
@@ -31,17 +36,17 @@ __host__ __device__ static inline int logit_rows(int cap) { return (cap + 31) / 
 // their offsets within a head travel in 32 bits
 static inline bool paged_logits_fit(int g, int cap) { return (long long)logit_rows(cap) * g < (1LL << 29); }
 
-// Whether every (sequence, KV head) goes to one workgroup that does all of it.
-constexpr int kWholeLogits = 5120;          // logits it keeps in LDS: 20 KB beside the merge area
-#ifndef WHOLE_PAIRS
-#define WHOLE_PAIRS 512
-#define WHOLE_ROWS 512
-#endif
+// Whether every (sequence, KV head) goes to one workgroup that does all of it, in one launch.  Short caches, where the second launch costs
+// more than a few tiles one after the other (2 heads of 200 rows: 3.9 us against 9.5; 8 of 700: 12.8 against 11.6; 8 of 2000: 29.5
+// against 11.4), and so many heads that they fill the chip as they are, as long as their logits fit LDS (1600 heads of up to 1200 rows
+// with weights: 68 us against 75; 512 of 4000 without: the same).
+constexpr int kWholeRows = 512, kWholePairs = 512;
+constexpr int kWholeLogits = 5120;          // 20 KB beside the merge area
 static inline bool paged_whole_heads(int S, int Hkv, int Hq, int cap, bool weights)
 {
     const int g = Hq / Hkv;
     if (weights && (g > kPagedQueries || (long long)(logit_rows(cap) + 4) * g > kWholeLogits)) return false;
-    return cap <= WHOLE_ROWS || ((long long)S * Hkv >= WHOLE_PAIRS && cap <= kWholeLogits);
+    return cap <= kWholeRows || ((long long)S * Hkv >= kWholePairs && cap <= kWholeLogits);
 }
 
 struct PagedAttendSpace {
@@ -51,7 +56,7 @@ static inline PagedAttendSpace paged_attend_space(bool bf16, int S, int Hkv, int
 {
     PagedAttendSpace p;
     const int g = Hq / Hkv, gt = g < kPagedQueries ? g : kPagedQueries;
-    const size_t slots = 2 * (size_t)paged_groups(bf16, S, Hkv, Hq, cap);
+    const size_t slots = 2 * (size_t)paged_groups(bf16, S, Hkv, Hq, cap, d);
     p.start = 256;
     p.stats = p.start + round_up((size_t)S * Hkv * paged_query_tiles(g) * sizeof(int32_t), 256);
     p.slot_stats = p.stats + round_up((size_t)S * Hq * sizeof(float), 256);
