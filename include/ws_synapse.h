@@ -344,7 +344,7 @@ typedef struct {
     void *K, *V;              /* dev [pages, Hkv, page, d] each, 16-byte aligned */
     const int32_t *table;     /* dev [S, per_seq] page numbers */
     const int32_t *len;       /* dev [S] rows in use */
-    ws_dtype dt;
+    int dt;                   /* a ws_dtype, of K and V */
     int pages, Hkv, page, d;  /* page: 16, 32, 64, 128 or 256 rows; d: 64 or 128 */
     int S, per_seq;           /* per_seq * page < 2^24 */
 } ws_paged_cache;
@@ -373,7 +373,8 @@ typedef struct {
  *              seen[s] - n + (t - first[s]), which stay with a row when an eviction moves it
  *   seen       dev [S] tokens the sequence has had so far, this append included (len while nothing was evicted); NULL with stamp NULL
  *   mass       dev [S, Hkv, per_seq * page] fp32 or NULL: the new rows' accounts, set to 0
- * A new row must not be shared between sequences, and q_out must not overlap k, v or q.  Rows outside the table are left out.
+ * A new row must not be shared between sequences.  q_out may be q itself where that is dense, and overlaps nothing else.  Rows outside
+ * the table are left out.
  */
 ws_status ws_synapse_paged_append(const ws_paged_cache *cache, const ws_rows *k, const ws_rows *v, int T, const int32_t *first,
                                   const int32_t *pos, int axes, const int *pairs_host, float base, const ws_rows *q, int Hq,
@@ -387,7 +388,7 @@ ws_status ws_synapse_paged_append(const ws_paged_cache *cache, const ws_rows *k,
  * A sequence of no rows gives O = 0 and lse = -infinity.  The cache is split over the device by its rows, whatever their
  * sequence, and joined; the same call on the same device gives the same bits.
  *   Q dev [S, Hq, d] dtype of the cache, already rotated;  Hq % Hkv == 0;  scale <= 0 means 1/sqrt(d)
- *   O dev [S, Hq, d] fp32;  lse dev [S, Hq] fp32 or NULL
+ *   O dev [S, Hq, d] fp32;  lse dev [S, Hq] fp32 or NULL;  workspace may be NULL when the reported size is 0 (short caches)
  *   mass_out dev [S, Hkv, per_seq * page] fp32 or NULL: no weights;  mass_in the same or NULL: from 0 on;  mass_in may be mass_out.
  *   Entries of rows behind len[s] are left as they are.  decay finite, >= 0 (1: a plain sum).
  *   The accounts are kept by sequence, not by page, so sequences that share pages have accounts of their own.
@@ -398,7 +399,8 @@ ws_status ws_synapse_paged_attend(const ws_paged_cache *cache, const void *Q, in
 /*
  * Every KV head of every sequence with more than `keep` rows gives up the ones with the least on their account, down to `keep`.
  * Rows with stamp < sinks or stamp >= seen[s] - recent are protected and stay; of the others those with the largest mass stay, of
- * equal ones those in the lowest row (a NaN counts as the least).  Stays that lie in the first `keep` rows are not moved; the
+ * equal ones those in the lowest row (a NaN counts as the least; of more than `keep` protected ones, which stamps that differ do not
+ * give, the lowest stay).  Stays that lie in the first `keep` rows are not moved; the
  * others fill the rows that became free below `keep`, in order: the i-th of them goes to the i-th free row.  (Attention does not
  * depend on the rows' order; moving no more than this is what the stamps are for.)  K, V, mass and stamp move together.
  *   seen      dev [S] as for the append;  sinks, recent >= 0, sinks + recent <= keep, keep >= 1

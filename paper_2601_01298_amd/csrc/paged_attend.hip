@@ -68,6 +68,48 @@ __device__ __forceinline__ int share_owner(int total, int groups, int t)
     return t < (per + 1) * rest ? t / (per + 1) : rest + (t - (per + 1) * rest) / per;
 }
 
+// A workgroup's run of units of UNIT rows, counted through all sequences and the `pairs` heads of each: units [from, to) of `total`, the
+// sequence s that holds unit `from`, and that sequence's first unit.  Every wave finds it for itself: a lane counts the units of some
+// consecutive sequences, a scan over the lanes gives where each lane's begin.
+struct Run {
+    int total, from, to, s, first;
+    template <int UNIT>
+    __device__ __forceinline__ void find(const AttendArgs &a, int pairs, int groups, int b)
+    {
+        const int lane = threadIdx.x & 63, cap = a.per_seq << a.page_shift, each = (a.S + 63) / 64;
+        int mine = 0;
+        for (int i = 0; i < each; ++i) {
+            const int q = lane * each + i;
+            if (q < a.S) mine += (paged_rows(a.len[q], cap) + UNIT - 1) / UNIT;
+        }
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(upto, o);
+            if (lane >= o) upto += y;
+        }
+        total = __builtin_amdgcn_readlane(upto, 63) * pairs;
+        from = share_start(total, groups, b);
+        to = share_start(total, groups, b + 1);
+        if (from >= to) return;
+        const int l = __builtin_ctzll(__ballot((long long)upto * pairs > from));        // the lane that reaches beyond `from`
+        s = l * each;
+        first = (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l)) * pairs;
+        skip<UNIT>(a, pairs, from);
+    }
+    // On to the sequence that holds unit t, which is not before s.
+    template <int UNIT>
+    __device__ __forceinline__ int skip(const AttendArgs &a, int pairs, int t)
+    {
+        for (;;) {
+            const int n = paged_rows(as_scalar(a.len)[s], a.per_seq << a.page_shift), units = (n + UNIT - 1) / UNIT;
+            if (t < first + units * pairs) return n;
+            first += units * pairs;
+            ++s;
+        }
+    }
+};
+
 template <bool BF16, int D>
 struct Shape {
     static constexpr int TR = BF16 ? 32 : 16;            // rows of a tile
@@ -89,7 +131,7 @@ constexpr int kNowhere = 0, kToMemory = 1, kToLds = 2;       // where the logits
 
 // Room for the four waves' parts of a result; a row's length shifts the banks from query to query.
 template <int D>
-struct Merge {
+struct alignas(16) Merge {
     float part[4][kPagedQueries][D + 4];
     float m[4][kPagedQueries], l[4][kPagedQueries];
     // the four parts of query q brought to their maximum: that, their sum of weights, and element e
@@ -365,58 +407,22 @@ paged_split(AttendArgs a)
 {
     constexpr int TR = Shape<BF16, D>::TR;
     __shared__ Merge<D> red;
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int b = blockIdx.x, groups = gridDim.x;
-    const int cap = a.per_seq << a.page_shift;
-    const int pairs = a.H * a.tiles_q;                   // of one sequence
-    const int g = a.Hq / a.H;
+    const int tid = threadIdx.x, b = blockIdx.x, groups = gridDim.x;
+    const int pairs = a.H * a.tiles_q, g = a.Hq / a.H;   // pairs: of one sequence
 
-    // ---- this workgroup's run of tiles, and the sequence it starts in.  Every wave finds them for itself: a lane counts the
-    // tiles of some consecutive sequences, a scan over the lanes gives the sequence's first tile.
-    const int each = (a.S + 63) / 64;
-    int mine = 0;
-    for (int i = 0; i < each; ++i) {
-        const int s = lane * each + i;
-        if (s < a.S) mine += (paged_rows(a.len[s], cap) + TR - 1) / TR;
-    }
-    int upto = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(upto, o);
-        if (lane >= o) upto += y;
-    }
-    const int total = __builtin_amdgcn_readlane(upto, 63) * pairs;
-    if (b == 0 && tid == 0) *a.total = total;
-    int t0 = share_start(total, groups, b);
-    const int t1 = share_start(total, groups, b + 1);
+    Run run;
+    run.template find<TR>(a, pairs, groups, b);
+    if (b == 0 && tid == 0) *a.total = run.total;
+    int t0 = run.from, s = run.s, first = run.first;
+    const int t1 = run.to;
     if (t0 >= t1) return;
-    int s, first;                                        // first tile of sequence s
-    {
-        // the first lane whose sequences reach beyond t0
-        const unsigned long long reach = __ballot((long long)upto * pairs > t0);
-        const int l = __builtin_ctzll(reach);
-        s = l * each;
-        first = (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l)) * pairs;
-        for (;;) {
-            const int ts = (paged_rows(as_scalar(a.len)[s], cap) + TR - 1) / TR * pairs;
-            if (t0 < first + ts) break;
-            first += ts;
-            ++s;
-        }
-    }
     // ---- its parts of pairs, one after the other; a part's first tile is asked for before the one before it is put together
     const int run0 = t0;
     Sweep<BF16, D, WEIGHTS ? kToMemory : kNowhere> w(a, nullptr, 0);
     int pair, pair0, ts;                                 // the part at t0: its pair within the sequence, the pair's first tile, its tiles
     auto begin = [&]() {
-        int n;
-        for (;;) {
-            n = paged_rows(as_scalar(a.len)[s], cap);
-            ts = (n + TR - 1) / TR;
-            if (ts != 0 && t0 < first + ts * pairs) break;
-            first += ts * pairs;
-            ++s;
-        }
+        const int n = run.template skip<TR>(a, pairs, t0);
+        s = run.s, first = run.first, ts = (n + TR - 1) / TR;
         pair = (t0 - first) / ts;
         pair0 = first + pair * ts;
         w.begin(s, pair / a.tiles_q, pair % a.tiles_q * kPagedQueries, n, t0 - pair0, min(ts, t1 - pair0));
@@ -487,7 +493,7 @@ paged_whole(AttendArgs a, int kept_stride)
     constexpr int TR = Shape<BF16, D>::TR;
     __shared__ Merge<D> red;
     __shared__ float stat[kPagedQueries];
-    extern __shared__ float kept[];                      // [g][kept_stride] logits
+    extern __shared__ __attribute__((aligned(16))) float kept[];     // [g][kept_stride] logits
     const int tid = threadIdx.x;
     const int cap = a.per_seq << a.page_shift, g = a.Hq / a.H;
     const int qt = blockIdx.x % a.tiles_q, pair = blockIdx.x / a.tiles_q, s = pair / a.H, h = pair % a.H;
@@ -596,18 +602,15 @@ __device__ void join_row(const AttendArgs &a, int groups, int row)
     if (tid == 0 && a.lse != nullptr) a.lse[row] = (m + __builtin_amdgcn_logf(l)) * 0.693147180559945309f;
 }
 
-// One workgroup per 1024 rows of a (sequence, KV head): what the rows received is added to their accounts.
+// 1024 rows of a (sequence, KV head): what the rows received is added to their accounts.
+constexpr int kWeightRows = 1024;
 template <bool BF16, int D>
-__device__ void add_weights(const AttendArgs &a, int groups, int pair, int chunk)
+__device__ __forceinline__ void add_weights(const AttendArgs &a, int groups, int s, int h, int n, int chunk, float *stat)
 {
     constexpr int TR = Shape<BF16, D>::TR;
-    __shared__ float stat[256];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int cap = a.per_seq << a.page_shift;
-    const int s = pair / a.H, h = pair % a.H, g = a.Hq / a.H;
-    const int n = paged_rows(a.len[s], cap);
-    if (chunk * 1024 >= n) return;
-    const int r = chunk * 1024 + tid * 4;
+    const int cap = a.per_seq << a.page_shift, g = a.Hq / a.H, pair = s * a.H + h;
+    const int r = chunk * kWeightRows + tid * 4;
     const float *z = a.logits + ((long long)pair * logit_rows(cap) + r / 16 * 16) * g + r % 16;
     f32x4_t w = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int q0 = 0; q0 < g; q0 += 256) {
@@ -642,14 +645,25 @@ __device__ void add_weights(const AttendArgs &a, int groups, int pair, int chunk
     if (r < n) account(a, (long long)pair * cap, r, n, w);
 }
 
+// The first S * Hq workgroups join, a query head of a sequence each; the others share out the rows whose weights are wanted.
 template <bool BF16, int D>
 __global__ void __launch_bounds__(256)
-paged_finish(AttendArgs a, int groups, int chunks)
+paged_finish(AttendArgs a, int groups)
 {
-    const long long b = blockIdx.x + (long long)blockIdx.y * gridDim.x;
     const int rows = a.S * a.Hq;
-    if (b < rows) join_row<BF16, D>(a, groups, (int)b);
-    else if (b - rows < (long long)a.S * a.H * chunks) add_weights<BF16, D>(a, groups, (int)((b - rows) / chunks), (int)((b - rows) % chunks));
+    if ((int)blockIdx.x < rows) {
+        join_row<BF16, D>(a, groups, blockIdx.x);
+        return;
+    }
+    __shared__ float stat[256];
+    Run run;
+    run.template find<kWeightRows>(a, a.H, gridDim.x - rows, blockIdx.x - rows);
+    for (int u = run.from; u < run.to; ++u) {
+        const int n = run.template skip<kWeightRows>(a, a.H, u), chunks = (n + kWeightRows - 1) / kWeightRows;
+        const int h = (u - run.first) / chunks;
+        add_weights<BF16, D>(a, groups, run.s, h, n, u - run.first - h * chunks, stat);
+        __syncthreads();
+    }
 }
 
 }  // namespace
@@ -690,10 +704,10 @@ hipError_t launch_paged_attend(const ws_paged_cache &c, const void *Q, int Hq, f
         else hipLaunchKernelGGL((paged_split<B, D, false>), grid, block, 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        const int chunks = mass_out ? (cap + 1023) / 1024 : 0;
-        const long long blocks = (long long)c.S * Hq + (long long)c.S * c.Hkv * chunks;
-        const unsigned x = blocks < (1 << 22) ? (unsigned)blocks : 1u << 22;
-        hipLaunchKernelGGL((paged_finish<B, D>), dim3(x, (unsigned)((blocks + x - 1) / x)), block, 0, st, a, groups, chunks);
+        // The lengths are on the device: of a long table most may be empty, and no launch is made of workgroups that find nothing to do.
+        const long long chunks = mass_out ? (long long)c.S * c.Hkv * ((cap + kWeightRows - 1) / kWeightRows) : 0;
+        const unsigned weighing = (unsigned)(chunks < 2048 ? chunks : 2048);
+        hipLaunchKernelGGL((paged_finish<B, D>), dim3((unsigned)(c.S * Hq) + weighing), block, 0, st, a, groups);
         return hipGetLastError();
     };
     using std::integral_constant;

@@ -7,7 +7,7 @@
 // listed in order, and row i of one list goes to row i of the other.
 //
 //   evict_pick   one workgroup per head, keys in registers: up to kPickRows rows.  With few moves it makes them too.
-//   evict_digit (three times), evict_count, evict_place   the same over workgroups of kChunk rows each, for longer heads: a step
+//   evict_chunks (five times)   the same over workgroups of kChunk rows each, for longer heads: a step
 //                that needs all chunks of a head (the counts of a digit, the rows listed before a chunk's) starts with a new
 //                launch and adds up what the chunks left, so nothing waits inside a kernel and nothing is added atomically
 //                between workgroups.
@@ -320,15 +320,11 @@ __device__ __forceinline__ int digit_of_chunks(const EvictArgs &a, int d, int pa
 }
 
 template <int DIGIT>
-__global__ void __launch_bounds__(256)
-evict_digit(EvictArgs a)
+__device__ __forceinline__ void digit_of_chunk(const EvictArgs &a, int pair, int n, int chunks, int chunk)
 {
     __shared__ uint32_t hist[kBins];
     __shared__ uint32_t wave_sum[4], found[2];
-    const int tid = threadIdx.x, chunk = blockIdx.x, pair = blockIdx.y + blockIdx.z * gridDim.y;
-    if (pair >= a.S * a.H) return;
-    const int n = a.rows_of(pair / a.H), chunks = (n + kChunk - 1) / kChunk;
-    if (chunk >= chunks) return;
+    const int tid = threadIdx.x;
     const long long at = (long long)pair * a.cap();
     if (n <= a.keep) {
         if (DIGIT == 0)
@@ -381,15 +377,12 @@ evict_digit(EvictArgs a)
 }
 
 // Who stays: one bit per row, and how many per chunk.
-__global__ void __launch_bounds__(256)
-evict_count(EvictArgs a)
+__device__ __forceinline__ void count_chunk(const EvictArgs &a, int pair, int n, int chunks, int chunk)
 {
     __shared__ uint32_t wave_sum[4], found[2];
     __shared__ int wave_ties[4], wave_stays[2][4], before;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, chunk = blockIdx.x, pair = blockIdx.y + blockIdx.z * gridDim.y;
-    if (pair >= a.S * a.H) return;
-    const int n = a.rows_of(pair / a.H), chunks = (n + kChunk - 1) / kChunk;
-    if (chunk >= chunks || n <= a.keep) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (n <= a.keep) return;
     const long long at = (long long)pair * a.cap();
     uint32_t key[kChunkKeys];
 #pragma unroll
@@ -440,18 +433,14 @@ evict_count(EvictArgs a)
 }
 
 // The lists of free rows and of rows that move, in order, and the accounts of those that neither are.
-__global__ void __launch_bounds__(256)
-evict_place(EvictArgs a)
+__device__ __forceinline__ void place_chunk(const EvictArgs &a, int pair, int n, int chunks, int chunk)
 {
     __shared__ int wave_free[4], wave_move[4], start[3];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, chunk = blockIdx.x, pair = blockIdx.y + blockIdx.z * gridDim.y;
-    if (pair >= a.S * a.H) return;
-    const int n = a.rows_of(pair / a.H), chunks = (n + kChunk - 1) / kChunk;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if (n <= a.keep) {
         if (chunk == 0 && tid == 0) a.count[pair] = 0;
         return;
     }
-    if (chunk >= chunks) return;
     const unsigned long long *bits = a.bits + ((long long)pair * a.chunks + chunk) * (kChunk / 64) + wave * kChunkKeys;
     unsigned long long mask[kChunkKeys];
 #pragma unroll
@@ -524,6 +513,24 @@ evict_place(EvictArgs a)
     }
 }
 
+// The steps over chunks.  The lengths are on the device, so a grid made for the longest cache there can be would be mostly empty: a head has
+// gridDim.x workgroups, which take its chunks in turn.  STEP 0 to 2: the digits, 3: who stays, 4: the lists.
+template <int STEP>
+__global__ void __launch_bounds__(256)
+evict_chunks(EvictArgs a)
+{
+    const int pair = blockIdx.y + blockIdx.z * gridDim.y;
+    if (pair >= a.S * a.H) return;
+    const int n = a.rows_of(pair / a.H), chunks = (n + kChunk - 1) / kChunk;
+    if (STEP == 4 && n == 0 && blockIdx.x == 0 && threadIdx.x == 0) a.count[pair] = 0;
+    for (int chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
+        if constexpr (STEP < 3) digit_of_chunk<STEP>(a, pair, n, chunks, chunk);
+        else if constexpr (STEP == 3) count_chunk(a, pair, n, chunks, chunk);
+        else place_chunk(a, pair, n, chunks, chunk);
+        if (chunk + (int)gridDim.x < chunks) __syncthreads();
+    }
+}
+
 __global__ void __launch_bounds__(256)
 evict_move(EvictArgs a)
 {
@@ -582,12 +589,13 @@ hipError_t launch_paged_evict(const ws_paged_cache &c, int keep, int sinks, int 
             return hipGetLastError();
         }
     } else {
-        const dim3 grid((unsigned)a.chunks, (unsigned)y, (unsigned)z), block(256);
-        hipLaunchKernelGGL((evict_digit<0>), grid, block, 0, st, a);
-        hipLaunchKernelGGL((evict_digit<1>), grid, block, 0, st, a);
-        hipLaunchKernelGGL((evict_digit<2>), grid, block, 0, st, a);
-        hipLaunchKernelGGL(evict_count, grid, block, 0, st, a);
-        hipLaunchKernelGGL(evict_place, grid, block, 0, st, a);
+        const int share = 4096 / pairs > 1 ? 4096 / pairs : 1;
+        const dim3 grid((unsigned)(a.chunks < share ? a.chunks : share), (unsigned)y, (unsigned)z), block(256);
+        hipLaunchKernelGGL((evict_chunks<0>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((evict_chunks<1>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((evict_chunks<2>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((evict_chunks<3>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((evict_chunks<4>), grid, block, 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

@@ -67,7 +67,7 @@ static inline PagedAttendSpace paged_attend_space(bool bf16, int S, int Hkv, int
 }
 static inline size_t paged_attend_workspace_bytes(bool bf16, int S, int Hkv, int Hq, int cap, int d, bool weights)
 {
-    return paged_attend_space(bf16, S, Hkv, Hq, cap, d, weights).bytes;
+    return paged_whole_heads(S, Hkv, Hq, cap, weights) ? 0 : paged_attend_space(bf16, S, Hkv, Hq, cap, d, weights).bytes;
 }
 
 // Per KV head of a sequence: how many rows move, and from where to where.

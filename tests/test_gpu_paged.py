@@ -148,6 +148,14 @@ def test_attend_shared_pages(ws):
     run_attend(ws, c, 4)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attend_tables_with_room_for_far_more(ws, dtype):
+    """Tables of 20 480 and of 131 072 rows of which a few are in use: the rows counted are those there are."""
+    run_attend(ws, plain.Cache([700, 0, 1, 3000], 3, 64, 256, dtype, seed=11, per_seq=80), 2)
+    run_attend(ws, plain.Cache([5], 2, 128, 256, dtype, seed=11, per_seq=512), 1)
+    run_attend(ws, plain.Cache([1500] * 40, 8, 64, 64, dtype, seed=12, per_seq=2048), 1)
+
+
 def test_attend_repeats_its_bits(ws):
     c = plain.Cache([5000, 17, 300, 0, 2222], 4, 128, 64, BF16, seed=8)
     a, b = run_attend(ws, c, 4), run_attend(ws, c, 4)
@@ -297,8 +305,8 @@ def test_append_leaves_out_what_has_no_place(ws):
 
 
 # ---- eviction -------------------------------------------------------------------------------------------------------------
-def run_evict(ws, lens, H, d, page, dtype, keep, sinks=0, recent=0, mass="rand", in_place=False, want_kept=True, seed=0):
-    c = plain.Cache(lens, H, d, page, dtype, seed)
+def run_evict(ws, lens, H, d, page, dtype, keep, sinks=0, recent=0, mass="rand", in_place=False, want_kept=True, seed=0, per_seq=None):
+    c = plain.Cache(lens, H, d, page, dtype, seed, per_seq)
     gen, S = c.gen, len(lens)
     m = torch.rand((S, H, c.rows), generator=gen)
     if mass == "ties":
@@ -365,6 +373,17 @@ def test_evict_protects(ws, in_place, keep, sinks, recent):
 def test_evict_lengths(ws, n, keep, mass):
     run_evict(ws, [n, n // 2], 1, 64, 128, BF16, keep, 4, min(keep - 4, 64) if keep > 4 else 0, mass) if keep > 4 else \
         run_evict(ws, [n, n // 2], 1, 64, 128, BF16, keep, 1, 1, mass)
+
+
+@pytest.mark.parametrize("keep", [100, 5000])
+def test_evict_tables_with_room_for_far_more(ws, keep):
+    """Tables of 131 072 rows of which a few are in use: one chunk or two of each head, more heads than workgroups for every chunk."""
+    run_evict(ws, [0, 99, 101, 4097, 8200], 2, 64, 256, BF16, keep, 3, 20, "ties", per_seq=512)
+    run_evict(ws, [130] * 70, 4, 64, 256, BF16, keep, 3, 20, "rand", in_place=True, want_kept=False, per_seq=512)
+
+
+def test_evict_long_heads_with_fewer_workgroups_than_chunks(ws):
+    run_evict(ws, [16500] + [90] * 41, 24, 64, 256, BF16, 2500, 3, 20, "rand")
 
 
 def test_evict_many_heads(ws):

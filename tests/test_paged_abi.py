@@ -90,7 +90,7 @@ def test_append_refuses(b, kw, why):
     (dict(space=None), "WORKSPACE"), (dict(space=0x1010), "WORKSPACE"), (dict(size=16), "WORKSPACE"),
 ])
 def test_attend_refuses(b, kw, why):
-    assert attend(b, cache(b), **kw) == getattr(b, "WS_ERR_" + why)
+    assert attend(b, cache(b, per_seq=200), **kw) == getattr(b, "WS_ERR_" + why)
 
 
 @pytest.mark.parametrize("kw,why", [
@@ -107,6 +107,9 @@ def test_workspaces(b):
     size = lambda op, **kw: b.ws_synapse_workspace_bytes(op, b.WS_BF16, kw.pop("H", 8), kw.pop("L", 4096), kw.pop("d", 128), **kw)
     plain, weights = (size(b.WS_OP_PAGED_ATTEND, k=w, N=16, Hq=32) for w in (0, 1))
     assert 0 < plain < weights <= plain + 16 * 32 * 4096 * 4 + 4096
+    # short caches are one workgroup's and need nothing
+    assert size(b.WS_OP_PAGED_ATTEND, k=0, N=16, Hq=32, L=512) == 0 < size(b.WS_OP_PAGED_ATTEND, k=0, N=16, Hq=32, L=528)
+    assert size(b.WS_OP_PAGED_ATTEND, k=1, N=100, Hq=8, L=1200) == 0
     assert size(b.WS_OP_PAGED_EVICT, k=100, N=16) >= 16 * 8 * 100 * 8
     for op, kw in ((b.WS_OP_PAGED_ATTEND, dict(N=16, Hq=30)), (b.WS_OP_PAGED_ATTEND, dict(N=0, Hq=32)), (b.WS_OP_PAGED_ATTEND, dict(N=16, Hq=0)),
                    (b.WS_OP_PAGED_ATTEND, dict(N=1 << 20, Hq=32)), (b.WS_OP_PAGED_ATTEND, dict(N=1, Hq=8, L=1 << 24)), (b.WS_OP_PAGED_ATTEND, dict(N=1, Hq=8, d=96)),
