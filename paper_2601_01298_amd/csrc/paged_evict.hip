@@ -12,7 +12,8 @@
 //                launch and adds up what the chunks left, so nothing waits inside a kernel and nothing is added atomically
 //                between workgroups.
 //   evict_move   copies the rows of K and V, accounts and stamps from and to where the lists say.
-// Bound: HBM (the moved rows); for short heads the chain of barriers of evict_pick.
+// Bound: HBM (the moved rows: 8 heads of 131072 rows to 32768, 201 MB in 45 us, 4.4 TB/s); for short heads the chain of barriers of evict_pick
+// (1600 heads of 1056 rows to 1024: 21 us, 59 MB), for long ones the launches (five of 6.5 to 8 us).
 #include <type_traits>
 
 #include "paged_internal.h"
