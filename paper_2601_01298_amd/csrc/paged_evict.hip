@@ -7,13 +7,14 @@
 // listed in order, and row i of one list goes to row i of the other.
 //
 //   evict_pick   one workgroup per head, keys in registers: up to kPickRows rows.  With few moves it makes them too.
-//   evict_chunks (five times)   the same over workgroups of kChunk rows each, for longer heads: a step
+//   evict_chunks (four times)   the same over workgroups of kChunk rows each, for longer heads: a step
 //                that needs all chunks of a head (the counts of a digit, the rows listed before a chunk's) starts with a new
 //                launch and adds up what the chunks left, so nothing waits inside a kernel and nothing is added atomically
 //                between workgroups.
 //   evict_move   copies the rows of K and V, accounts and stamps from and to where the lists say.
 // Bound: HBM (the moved rows: 8 heads of 131072 rows to 32768, 201 MB in 45 us, 4.4 TB/s); for short heads the chain of barriers of evict_pick
-// (1600 heads of 1056 rows to 1024: 21 us, 59 MB), for long ones the launches (five of 6.5 to 8 us).
+// (1600 heads of 1056 rows to 1024: 21 us, 59 MB), for long ones the launches (7.2, 7.6, 7.7
+// and 12.5 us).
 #include <type_traits>
 
 #include "paged_internal.h"
@@ -40,9 +41,8 @@ struct EvictArgs {
     int most, chunks;
     uint32_t *keys;                         // [pairs][cap]
     uint16_t *hist;                         // [3][pairs][chunks][kBins]
-    uint2 *cells;                           // [3][pairs]: the digits found so far, and how many rows with exactly them are kept
-    int2 *chunk_stays;                      // [pairs][chunks]: rows that stay, below `keep` and behind it
-    unsigned long long *bits;               // [pairs][chunks][kChunk / 64]: who stays
+    uint2 *cells;                           // [2][pairs]: the digits found so far, and how many rows with exactly them are kept
+    int32_t *above;                         // [pairs][chunks]: keys above all that start with the first two digits
     __device__ int rows_of(int s) const { return paged_rows(len[s], per_seq << page_shift); }
     __device__ int cap() const { return per_seq << page_shift; }
     __device__ uint16_t *hist_of(int digit, int pair, int chunk) const
@@ -292,7 +292,18 @@ evict_lengths(EvictArgs a)
 // ---- heads of more rows: a workgroup per chunk ------------------------------------------------------------------------------
 constexpr int kChunkKeys = kChunk / 256;    // per thread
 
-__device__ __forceinline__ int chunk_row(int chunk, int k) { return chunk * kChunk + (threadIdx.x >> 6) * (kChunk / 4) + k * 64 + (threadIdx.x & 63); }
+// The rows of a head in chunks: first those below `keep`, then those behind, so that a chunk has rows of one kind only.
+struct Chunks {
+    int n, keep, low, all;                  // chunks below `keep`, chunks
+    __device__ __forceinline__ Chunks(int rows, int k)
+        : n(rows), keep(k), low((min(rows, k) + kChunk - 1) / kChunk), all(low + (max(0, rows - k) + kChunk - 1) / kChunk)
+    {
+    }
+    __device__ __forceinline__ int base(int c) const { return c < low ? c * kChunk : keep + (c - low) * kChunk; }
+    __device__ __forceinline__ int end(int c) const { return min(c < low ? min(keep, n) : n, base(c) + kChunk); }
+};
+// Row k of a thread in the chunk that starts at `base`: the order of rows is the order of waves, runs of 64 and lanes.
+__device__ __forceinline__ int chunk_row(int base, int k) { return base + (threadIdx.x >> 6) * (kChunk / 4) + k * 64 + (threadIdx.x & 63); }
 
 // The value of digit `d` from the counts that all chunks of the head left; `left` as in find_digit.
 template <int BINS>
@@ -321,18 +332,19 @@ __device__ __forceinline__ int digit_of_chunks(const EvictArgs &a, int d, int pa
 }
 
 template <int DIGIT>
-__device__ __forceinline__ void digit_of_chunk(const EvictArgs &a, int pair, int n, int chunks, int chunk)
+__device__ __forceinline__ void digit_of_chunk(const EvictArgs &a, int pair, const Chunks &chunks, int chunk)
 {
     __shared__ uint32_t hist[kBins];
     __shared__ uint32_t wave_sum[4], found[2];
-    const int tid = threadIdx.x;
+    __shared__ int wave_above[4];
+    const int tid = threadIdx.x, base = chunks.base(chunk), end = chunks.end(chunk);
     const long long at = (long long)pair * a.cap();
-    if (n <= a.keep) {
+    if (chunks.n <= a.keep) {
         if (DIGIT == 0)
 #pragma unroll 8
             for (int k = 0; k < kChunkKeys; ++k) {
-                const int i = chunk_row(chunk, k);
-                if (i < n) leave_row(a, pair, i, a.mass_in[at + i], a.stamp_in[at + i]);
+                const int i = chunk_row(base, k);
+                if (i < end) leave_row(a, pair, i, a.mass_in[at + i], a.stamp_in[at + i]);
             }
         return;
     }
@@ -343,7 +355,7 @@ __device__ __forceinline__ void digit_of_chunk(const EvictArgs &a, int pair, int
         int stamp[kChunkKeys];
 #pragma unroll
         for (int k = 0; k < kChunkKeys; ++k) {
-            const int i = min(chunk_row(chunk, k), n - 1);
+            const int i = min(chunk_row(base, k), end - 1);
             mass[k] = a.mass_in[at + i];
             stamp[k] = a.stamp_in[at + i];
         }
@@ -351,7 +363,7 @@ __device__ __forceinline__ void digit_of_chunk(const EvictArgs &a, int pair, int
         for (int k = 0; k < kChunkKeys; ++k) key[k] = key_of(mass[k], stamp[k], a.sinks, fresh);
     } else {
 #pragma unroll
-        for (int k = 0; k < kChunkKeys; ++k) key[k] = a.keys[at + min(chunk_row(chunk, k), n - 1)];
+        for (int k = 0; k < kChunkKeys; ++k) key[k] = a.keys[at + min(chunk_row(base, k), end - 1)];
     }
     for (int i = tid; i < kBins; i += 256) hist[i] = 0;
     uint32_t prefix = 0, left = (uint32_t)a.keep;
@@ -360,7 +372,7 @@ __device__ __forceinline__ void digit_of_chunk(const EvictArgs &a, int pair, int
             const uint2 cell = a.cells[pair];
             prefix = cell.x, left = cell.y;
         }
-        prefix |= (uint32_t)digit_of_chunks<kBins>(a, DIGIT - 1, pair, chunks, left, wave_sum, found) << (DIGIT == 1 ? 21 : 10);
+        prefix |= (uint32_t)digit_of_chunks<kBins>(a, DIGIT - 1, pair, chunks.all, left, wave_sum, found) << (DIGIT == 1 ? 21 : 10);
         if (chunk == 0 && tid == 0) a.cells[(long long)(DIGIT - 1) * a.S * a.H + pair] = make_uint2(prefix, left);
     }
     __syncthreads();
@@ -368,167 +380,140 @@ __device__ __forceinline__ void digit_of_chunk(const EvictArgs &a, int pair, int
     constexpr uint32_t KNOWN = DIGIT == 0 ? 0u : DIGIT == 1 ? 0xFFFFFFFFu << 21 : 0xFFFFFFFFu << 10;
 #pragma unroll
     for (int k = 0; k < kChunkKeys; ++k)
-        if (chunk_row(chunk, k) < n) {
-            if (DIGIT == 0) a.keys[at + chunk_row(chunk, k)] = key[k];
+        if (chunk_row(base, k) < end) {
+            if (DIGIT == 0) a.keys[at + chunk_row(base, k)] = key[k];
             if ((key[k] & KNOWN) == prefix) atomicAdd(&hist[(key[k] >> SHIFT) & ((1 << kDigits[DIGIT]) - 1)], 1u);
         }
+    if constexpr (DIGIT == 2) {
+        int more = 0;
+#pragma unroll
+        for (int k = 0; k < kChunkKeys; ++k) more += __popcll(__ballot(chunk_row(base, k) < end && key[k] > (prefix | 1023u)));
+        if ((tid & 63) == 0) wave_above[tid >> 6] = more;
+    }
     __syncthreads();
+    if (DIGIT == 2 && tid == 0) a.above[(long long)pair * a.chunks + chunk] = wave_above[0] + wave_above[1] + wave_above[2] + wave_above[3];
     uint32_t *out = reinterpret_cast<uint32_t *>(a.hist_of(DIGIT, pair, chunk));
     for (int i = tid; i < (1 << kDigits[DIGIT]) / 2; i += 256) out[i] = hist[2 * i] | hist[2 * i + 1] << 16;
 }
 
-// Who stays: one bit per row, and how many per chunk.
-__device__ __forceinline__ void count_chunk(const EvictArgs &a, int pair, int n, int chunks, int chunk)
+// Who stays, the lists of free rows and of rows that move, in order, and the accounts of those that are neither.  Of the chunks before
+// this one no more is needed than how many of their keys lie above the threshold and how many at it: of the latter the first `left` of the
+// head stay, so min(left, how many there were) of them have.
+__device__ __forceinline__ void place_chunk(const EvictArgs &a, int pair, const Chunks &chunks, int chunk)
 {
     __shared__ uint32_t wave_sum[4], found[2];
-    __shared__ int wave_ties[4], wave_stays[2][4], before;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    if (n <= a.keep) return;
-    const long long at = (long long)pair * a.cap();
-    uint32_t key[kChunkKeys];
-#pragma unroll
-    for (int k = 0; k < kChunkKeys; ++k) key[k] = a.keys[at + min(chunk_row(chunk, k), n - 1)];
-    const uint2 cell = a.cells[(long long)a.S * a.H + pair];
-    uint32_t left = cell.y;
-    const int digit = digit_of_chunks<kBins / 2>(a, 2, pair, chunks, left, wave_sum, found);
-    const uint32_t prefix = cell.x | (uint32_t)digit;
-    // equal keys in the chunks before this one
-    if (wave == 0) {
-        int sum = 0;
-        for (int c = lane; c < chunk; c += 64) sum += a.hist_of(2, pair, c)[digit];
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-        if (lane == 0) before = sum;
-    }
-    int ties = 0;
-#pragma unroll
-    for (int k = 0; k < kChunkKeys; ++k) ties += __popcll(__ballot(chunk_row(chunk, k) < n && key[k] == prefix));
-    if (lane == 0) wave_ties[wave] = ties;
-    __syncthreads();
-    ties = before;
-#pragma unroll
-    for (int w = 0; w < 3; ++w)
-        if (w < wave) ties += wave_ties[w];
-    int low = 0, high = 0;
-#pragma unroll
-    for (int k = 0; k < kChunkKeys; ++k) {
-        const int i = chunk_row(chunk, k);
-        const bool tie = i < n && key[k] == prefix;
-        const unsigned long long mask = __ballot(tie);
-        const bool stay = i < n && (key[k] > prefix || (tie && ties + below(mask) < (int)left));
-        ties += __popcll(mask);
-        const unsigned long long stays = __ballot(stay);
-        if (lane == 0) a.bits[((long long)pair * a.chunks + chunk) * (kChunk / 64) + wave * kChunkKeys + k] = stays;
-        low += __popcll(__ballot(stay && i < a.keep));
-        high += __popcll(__ballot(stay && i >= a.keep));
-    }
-    if (lane == 0) {
-        wave_stays[0][wave] = low;
-        wave_stays[1][wave] = high;
-    }
-    __syncthreads();
-    if (tid == 0)
-        a.chunk_stays[(long long)pair * a.chunks + chunk] =
-            make_int2(wave_stays[0][0] + wave_stays[0][1] + wave_stays[0][2] + wave_stays[0][3],
-                      wave_stays[1][0] + wave_stays[1][1] + wave_stays[1][2] + wave_stays[1][3]);
-}
-
-// The lists of free rows and of rows that move, in order, and the accounts of those that neither are.
-__device__ __forceinline__ void place_chunk(const EvictArgs &a, int pair, int n, int chunks, int chunk)
-{
-    __shared__ int wave_free[4], wave_move[4], start[3];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    if (n <= a.keep) {
+    __shared__ int sums[4][4], wave_ties[4], wave_listed[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, base = chunks.base(chunk), end = chunks.end(chunk);
+    if (chunks.n <= a.keep) {
         if (chunk == 0 && tid == 0) a.count[pair] = 0;
         return;
     }
-    const unsigned long long *bits = a.bits + ((long long)pair * a.chunks + chunk) * (kChunk / 64) + wave * kChunkKeys;
-    unsigned long long mask[kChunkKeys];
-#pragma unroll
-    for (int k = 0; k < kChunkKeys; ++k) mask[k] = bits[k];
+    const bool low = chunk < chunks.low, elsewhere = a.mass_out != a.mass_in || a.stamp_out != a.stamp_in;
+    const long long at = (long long)pair * a.cap();
+    uint32_t key[kChunkKeys];
     float mass[kChunkKeys];
     int stamp[kChunkKeys];
-    const bool elsewhere = a.mass_out != a.mass_in || a.stamp_out != a.stamp_in;
-    const long long at = (long long)pair * a.cap();
-    if (elsewhere && chunk * kChunk < a.keep)
+#pragma unroll
+    for (int k = 0; k < kChunkKeys; ++k) key[k] = a.keys[at + min(chunk_row(base, k), end - 1)];
+    if (low && elsewhere)
 #pragma unroll
         for (int k = 0; k < kChunkKeys; ++k) {
-            const int i = min(chunk_row(chunk, k), n - 1);
+            const int i = min(chunk_row(base, k), end - 1);
             mass[k] = a.mass_in[at + i];
             stamp[k] = a.stamp_in[at + i];
         }
-    if (wave == 0) {
-        int nfree = 0, nmove = 0, all = 0;
-        for (int c = lane; c < chunks; c += 64) {
-            const int2 stays = a.chunk_stays[(long long)pair * a.chunks + c];
-            const int gone = max(0, min(kChunk, a.keep - c * kChunk)) - stays.x;
-            all += gone;
-            if (c < chunk) {
-                nfree += gone;
-                nmove += stays.y;
+    const uint2 cell = a.cells[(long long)a.S * a.H + pair];
+    uint32_t left = cell.y;
+    const int digit = digit_of_chunks<kBins / 2>(a, 2, pair, chunks.all, left, wave_sum, found);
+    const uint32_t threshold = cell.x | (uint32_t)digit;
+    // keys above the threshold and at it in the chunks before this one, and in those below `keep`
+    int before[2] = {0, 0}, lower[2] = {0, 0};                   // of this lane's values of the last digit
+#pragma unroll 4
+    for (int c = wave; c < max(chunk, chunks.low); c += 4) {
+        const uint16_t *h = a.hist_of(2, pair, c);
+        int over = lane == 0 ? a.above[(long long)pair * a.chunks + c] : 0, equal = 0;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const uint4 x = reinterpret_cast<const uint4 *>(h)[2 * lane + half];
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int bin = 16 * lane + 8 * half + i, n = (int)((w[i / 2] >> (16 * (i & 1))) & 0xFFFFu);
+                if (bin > digit) over += n;
+                if (bin == digit) equal += n;
             }
         }
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            nfree += __shfl_xor(nfree, o);
-            nmove += __shfl_xor(nmove, o);
-            all += __shfl_xor(all, o);
-        }
-        if (lane == 0) {
-            start[0] = nfree;
-            start[1] = nmove;
-            if (chunk == 0) a.count[pair] = all;
-        }
+        if (c < chunk) before[0] += over, before[1] += equal;
+        if (c < chunks.low) lower[0] += over, lower[1] += equal;
     }
-    int nfree = 0, nmove = 0;
 #pragma unroll
-    for (int k = 0; k < kChunkKeys; ++k) {
-        const int i = chunk_row(chunk, k);
-        const bool stay = (mask[k] >> lane) & 1ull;
-        nfree += __popcll(__ballot(i < a.keep && !stay));
-        nmove += __popcll(__ballot(i >= a.keep && stay));
+    for (int o = 1; o < 64; o <<= 1) {
+        before[0] += __shfl_xor(before[0], o);
+        before[1] += __shfl_xor(before[1], o);
+        lower[0] += __shfl_xor(lower[0], o);
+        lower[1] += __shfl_xor(lower[1], o);
     }
+    int ties = 0;
+#pragma unroll
+    for (int k = 0; k < kChunkKeys; ++k) ties += __popcll(__ballot(chunk_row(base, k) < end && key[k] == threshold));
     if (lane == 0) {
-        wave_free[wave] = nfree;
-        wave_move[wave] = nmove;
+        sums[wave][0] = before[0], sums[wave][1] = before[1], sums[wave][2] = lower[0], sums[wave][3] = lower[1];
+        wave_ties[wave] = ties;
     }
     __syncthreads();
-    nfree = start[0], nmove = start[1];
+    int sum[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] = sums[0][i] + sums[1][i] + sums[2][i] + sums[3][i];
+    const int kept_before = sum[0] + min((int)left, sum[1]), kept_low = sum[2] + min((int)left, sum[3]);
+    if (chunk == 0 && tid == 0) a.count[pair] = a.keep - kept_low;
+    ties = sum[1];
 #pragma unroll
     for (int w = 0; w < 3; ++w)
-        if (w < wave) {
-            nfree += wave_free[w];
-            nmove += wave_move[w];
-        }
-    int32_t *free_rows = a.moves + (long long)pair * 2 * a.most, *movers = free_rows + a.most;
+        if (w < wave) ties += wave_ties[w];
+    uint32_t stays = 0;                                          // bit k: row k of this lane
+    int listed = 0;
 #pragma unroll
     for (int k = 0; k < kChunkKeys; ++k) {
-        const int i = chunk_row(chunk, k);
-        const bool stay = (mask[k] >> lane) & 1ull, is_free = i < a.keep && !stay, moves = i >= a.keep && stay;
-        const unsigned long long fm = __ballot(is_free), mm = __ballot(moves);
-        if (is_free) free_rows[nfree + below(fm)] = i;
-        if (moves) movers[nmove + below(mm)] = i;
-        nfree += __popcll(fm);
-        nmove += __popcll(mm);
-        if (stay && !moves) leave_row(a, pair, i, mass[k], stamp[k]);
+        const bool there = chunk_row(base, k) < end, tie = there && key[k] == threshold;
+        const unsigned long long mask = __ballot(tie);
+        const bool stay = there && (key[k] > threshold || (tie && ties + below(mask) < (int)left));
+        ties += __popcll(mask);
+        if (stay) stays |= 1u << k;
+        listed += __popcll(__ballot(there && stay != low));
+    }
+    if (lane == 0) wave_listed[wave] = listed;
+    __syncthreads();
+    // a chunk below `keep` lists those that go, a chunk behind it those that stay
+    listed = low ? chunk * kChunk - kept_before : kept_before - kept_low;
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+        if (w < wave) listed += wave_listed[w];
+    int32_t *list = a.moves + ((long long)pair * 2 + (low ? 0 : 1)) * a.most;
+#pragma unroll
+    for (int k = 0; k < kChunkKeys; ++k) {
+        const int i = chunk_row(base, k);
+        const bool there = i < end, stay = (stays >> k) & 1u, mine = there && stay != low;
+        const unsigned long long mask = __ballot(mine);
+        if (mine) list[listed + below(mask)] = i;
+        listed += __popcll(mask);
+        if (low && stay) leave_row(a, pair, i, mass[k], stamp[k]);
     }
 }
 
 // The steps over chunks.  The lengths are on the device, so a grid made for the longest cache there can be would be mostly empty: a head has
-// gridDim.x workgroups, which take its chunks in turn.  STEP 0 to 2: the digits, 3: who stays, 4: the lists.
+// gridDim.x workgroups, which take its chunks in turn.  STEP 0 to 2: the digits, 3: who stays, and the lists.
 template <int STEP>
 __global__ void __launch_bounds__(256)
 evict_chunks(EvictArgs a)
 {
     const int pair = blockIdx.y + blockIdx.z * gridDim.y;
     if (pair >= a.S * a.H) return;
-    const int n = a.rows_of(pair / a.H), chunks = (n + kChunk - 1) / kChunk;
-    if (STEP == 4 && n == 0 && blockIdx.x == 0 && threadIdx.x == 0) a.count[pair] = 0;
-    for (int chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
-        if constexpr (STEP < 3) digit_of_chunk<STEP>(a, pair, n, chunks, chunk);
-        else if constexpr (STEP == 3) count_chunk(a, pair, n, chunks, chunk);
-        else place_chunk(a, pair, n, chunks, chunk);
-        if (chunk + (int)gridDim.x < chunks) __syncthreads();
+    const Chunks chunks(a.rows_of(pair / a.H), a.keep);
+    if (STEP == 3 && chunks.all == 0 && blockIdx.x == 0 && threadIdx.x == 0) a.count[pair] = 0;
+    for (int chunk = blockIdx.x; chunk < chunks.all; chunk += gridDim.x) {
+        if constexpr (STEP < 3) digit_of_chunk<STEP>(a, pair, chunks, chunk);
+        else place_chunk(a, pair, chunks, chunk);
+        if (chunk + (int)gridDim.x < chunks.all) __syncthreads();
     }
 }
 
@@ -567,8 +552,7 @@ hipError_t launch_paged_evict(const ws_paged_cache &c, int keep, int sinks, int 
     a.keys = reinterpret_cast<uint32_t *>(base + sp.keys);
     a.hist = reinterpret_cast<uint16_t *>(base + sp.hist);
     a.cells = reinterpret_cast<uint2 *>(base + sp.cells);
-    a.chunk_stays = reinterpret_cast<int2 *>(base + sp.stays);
-    a.bits = reinterpret_cast<unsigned long long *>(base + sp.bits);
+    a.above = reinterpret_cast<int32_t *>(base + sp.above);
     const int y = pairs < 32768 ? pairs : 32768, z = (pairs + y - 1) / y;
     if (cap <= kPickRows) {
         const bool move = a.most <= kInlineMoves;
@@ -596,7 +580,6 @@ hipError_t launch_paged_evict(const ws_paged_cache &c, int keep, int sinks, int 
         hipLaunchKernelGGL((evict_chunks<1>), grid, block, 0, st, a);
         hipLaunchKernelGGL((evict_chunks<2>), grid, block, 0, st, a);
         hipLaunchKernelGGL((evict_chunks<3>), grid, block, 0, st, a);
-        hipLaunchKernelGGL((evict_chunks<4>), grid, block, 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

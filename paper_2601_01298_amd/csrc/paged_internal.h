@@ -74,9 +74,10 @@ static inline size_t paged_attend_workspace_bytes(bool bf16, int S, int Hkv, int
 static inline int paged_evict_moves(int cap, int keep) { return keep >= cap ? 1 : (keep < cap - keep ? keep : cap - keep); }
 constexpr int kPickRows = 16384;            // rows of a head whose choice one workgroup makes
 constexpr int kChunk = 4096;                // rows per workgroup of longer ones
-static inline int paged_evict_chunks(int cap) { return cap <= kPickRows ? 0 : (cap + kChunk - 1) / kChunk; }
+// (one more than the rows fill, because no chunk has rows on both sides of `keep`)
+static inline int paged_evict_chunks(int cap) { return cap <= kPickRows ? 0 : (cap + kChunk - 1) / kChunk + 1; }
 struct PagedEvictSpace {
-    size_t moves, keys, hist, cells, stays, bits, bytes;     // offsets, total; the counts of moves lie at 0
+    size_t moves, keys, hist, cells, above, bytes;           // offsets, total; the counts of moves lie at 0
 };
 static inline PagedEvictSpace paged_evict_space(int S, int Hkv, int cap, int keep)
 {
@@ -86,9 +87,8 @@ static inline PagedEvictSpace paged_evict_space(int S, int Hkv, int cap, int kee
     p.keys = p.moves + round_up(pairs * paged_evict_moves(cap, keep) * 2 * sizeof(int32_t), 256);
     p.hist = p.keys + (chunks ? round_up(pairs * cap * sizeof(uint32_t), 256) : 0);
     p.cells = p.hist + chunks * 3 * 2048 * sizeof(uint16_t);
-    p.stays = p.cells + (chunks ? round_up(pairs * 3 * 8, 256) : 0);
-    p.bits = p.stays + round_up(chunks * 8, 256);
-    p.bytes = p.bits + chunks * (kChunk / 8);
+    p.above = p.cells + (chunks ? round_up(pairs * 2 * 8, 256) : 0);
+    p.bytes = p.above + round_up(chunks * 4, 256);
     return p;
 }
 static inline size_t paged_evict_workspace_bytes(int S, int Hkv, int cap, int keep) { return paged_evict_space(S, Hkv, cap, keep).bytes; }
