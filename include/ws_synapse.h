@@ -339,6 +339,8 @@ ws_status ws_synapse_inject(void *Kc, void *Vc, ws_dtype dt, int H, int Lcap, in
  *   len counts what is there AFTER an append.  A value outside [0, per_seq * page] is clamped into range, a page number outside
  *   [0, pages) is not followed: an append or a move to such a page is left out, a row read from one counts as row of page 0.
  *   Table entries behind a sequence's last page in use are not read.  Rows behind a sequence's last one may hold anything (NaN too).
+ * A page may stand in several tables, and several times in one, as long as it is only read.
+ * S * Hkv and S * Hq are at most 2^20 (WS_ERR_UNSUPPORTED beyond).
  */
 typedef struct {
     void *K, *V;              /* dev [pages, Hkv, page, d] each, 16-byte aligned */
@@ -373,7 +375,7 @@ typedef struct {
  *              seen[s] - n + (t - first[s]), which stay with a row when an eviction moves it
  *   seen       dev [S] tokens the sequence has had so far, this append included (len while nothing was evicted); NULL with stamp NULL
  *   mass       dev [S, Hkv, per_seq * page] fp32 or NULL: the new rows' accounts, set to 0
- * A new row must not be shared between sequences.  q_out may be q itself where that is dense, and overlaps nothing else.  Rows outside
+ * The page of a new row must stand in one table only, and once.  q_out may be q itself where that is dense, and overlaps nothing else.  Rows outside
  * the table are left out.
  */
 ws_status ws_synapse_paged_append(const ws_paged_cache *cache, const ws_rows *k, const ws_rows *v, int T, const int32_t *first,
@@ -390,7 +392,8 @@ ws_status ws_synapse_paged_append(const ws_paged_cache *cache, const ws_rows *k,
  *   Q dev [S, Hq, d] dtype of the cache, already rotated;  Hq % Hkv == 0;  scale <= 0 means 1/sqrt(d)
  *   O dev [S, Hq, d] fp32;  lse dev [S, Hq] fp32 or NULL;  workspace may be NULL when the reported size is 0 (short caches)
  *   mass_out dev [S, Hkv, per_seq * page] fp32 or NULL: no weights;  mass_in the same or NULL: from 0 on;  mass_in may be mass_out.
- *   Entries of rows behind len[s] are left as they are.  decay finite, >= 0 (1: a plain sum).
+ *   Entries of rows behind len[s] are left as they are.  decay finite, >= 0 (1: a plain sum).  With weights per_seq * page * g stays
+ *   below 2^29, and the workspace holds a logit per query head and row of the tables.
  *   The accounts are kept by sequence, not by page, so sequences that share pages have accounts of their own.
  */
 ws_status ws_synapse_paged_attend(const ws_paged_cache *cache, const void *Q, int Hq, float scale, float *O, float *lse, float decay,
@@ -409,7 +412,7 @@ ws_status ws_synapse_paged_attend(const ws_paged_cache *cache, const void *Q, in
  *   len_out   dev [S], min(len, keep), written; may be cache->len
  *   kept      dev [S, Hkv, keep] int32 or NULL: the row each row below len_out[s] was before (entries behind left as they are)
  * Rows of K and V at `keep` and behind are left as they are, so the call can be made again with the same inputs.  A page in which rows
- * move must not be shared between sequences; rows that are protected from the first eviction on, at the head of the table, never move.
+ * move must stand in one table only, and once; rows that are protected from the first eviction on, at the head of the table, never move.
  */
 ws_status ws_synapse_paged_evict(const ws_paged_cache *cache, int keep, int sinks, int recent, const int32_t *seen,
                                  const float *mass_in, float *mass_out, const int32_t *stamp_in, int32_t *stamp_out,

@@ -68,6 +68,19 @@ def test_attend_with_many_query_heads(ws, dtype, g):
     run_attend(ws, plain.Cache([70, 0, 300, 1, 129], 1, 128, 16, dtype, seed=g), g, weights=False)
 
 
+def test_attend_with_hundreds_of_query_heads_per_key_head(ws):
+    run_attend(ws, plain.Cache([70, 0, 600, 1], 1, 64, 64, BF16, seed=3), 261)
+
+
+@pytest.mark.parametrize("dtype,d,g", [(BF16, 64, 1), (BF16, 128, 4), (F32, 64, 3)])
+def test_attend_with_as_many_heads_as_fill_the_chip(ws, dtype, d, g):
+    """512 and more (sequence, head) pairs whose logits fit LDS: a workgroup each, rows up to 1216."""
+    rng = np.random.default_rng(g)
+    lens = [int(n) for n in rng.integers(0, 1217, 69)] + [1216]
+    run_attend(ws, plain.Cache(lens, 8, d, 32, dtype, seed=g), g)
+    run_attend(ws, plain.Cache([3 * n for n in lens], 8, d, 32, dtype, seed=g), g, weights=False)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("before", ["rand", "none", "same"])
 def test_attend_accounts(ws, dtype, before):
@@ -475,6 +488,51 @@ def test_agents_decode_over_a_shared_synapse(ws):
                     assert stamp[a, h, :budget].tolist() == [x[2] for x in ref[a][h]]
                     assert came[:k_used] == list(range(k_used))
     assert evictions >= 4
+
+
+def test_two_batches_at_once_on_two_streams(ws):
+    """Two caches, two streams, a workspace each: attention and eviction of both in flight together, the same bits as one after the
+    other (long enough for the calls to overlap: splits, joins, long heads over chunks)."""
+    torch.manual_seed(0)
+    sets = []
+    for i in range(2):
+        H, d, page, rows = 8, 128, 64, 20480
+        K = torch.randn((2 * rows // page, H, page, d), device="cuda").to(BF16)
+        V = torch.randn_like(K)
+        table = torch.randperm(2 * rows // page, device="cuda").to(torch.int32).view(2, -1).contiguous()
+        cache = ws.PagedCache(K, V, table, torch.tensor([rows - 37 * i, rows - 1000], dtype=torch.int32, device="cuda"))
+        mass = torch.rand((2, H, rows), device="cuda")
+        sets.append(dict(cache=cache, Q=torch.randn((2, 32, d), device="cuda").to(BF16), mass=mass, out=torch.zeros_like(mass),
+                         O=torch.zeros((2, 32, d), device="cuda"), seen=cache.len + 5, mass2=torch.zeros_like(mass),
+                         stamp=torch.arange(rows, dtype=torch.int32, device="cuda").expand(2, H, rows).contiguous(),
+                         stamp2=torch.zeros((2, H, rows), dtype=torch.int32, device="cuda"), len2=torch.zeros_like(cache.len), K0=K.clone(), V0=V.clone(),
+                         wa=ws.ws_synapse_paged_workspace(cache, "attend", 32, True), we=ws.ws_synapse_paged_workspace(cache, "evict", keep=9000)))
+
+    def go(s, stream=None):
+        ws.ws_synapse_paged_attend(s["cache"], s["Q"], O=s["O"], decay=0.5, mass_in=s["mass"], mass_out=s["out"], workspace=s["wa"], stream=stream)
+        ws.ws_synapse_paged_evict(s["cache"], 9000, s["seen"], s["out"], s["stamp"], 4, 100, mass_out=s["mass2"], stamp_out=s["stamp2"],
+                                  len_out=s["len2"], workspace=s["we"], stream=stream)
+
+    results = lambda s: [s[n].clone() for n in ("O", "out", "mass2", "stamp2", "len2")] + [s["cache"].K.clone(), s["cache"].V.clone()]
+    want = []
+    for s in sets:
+        go(s)
+        torch.cuda.synchronize()
+        want.append(results(s))
+        assert s["len2"].tolist() == [9000, 9000]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for again in range(3):
+        for s in sets:
+            s["cache"].K.copy_(s["K0"])
+            s["cache"].V.copy_(s["V0"])
+            for n in ("O", "out", "mass2", "stamp2", "len2"):
+                s[n].zero_()
+        torch.cuda.synchronize()
+        for s, stream in zip(sets, streams):
+            go(s, stream)
+        torch.cuda.synchronize()
+        for s, w in zip(sets, want):
+            assert all(torch.equal(a, b) for a, b in zip(results(s), w))
 
 
 def test_a_step_in_a_graph_and_on_another_stream(ws):
