@@ -573,15 +573,29 @@ __device__ void join_row(const AttendArgs &a, int groups, int row)
     }
     const Parts p = parts_of<TR>(a, groups, s, h, q, n);
     if (p.b0 == p.b1) return;                            // one workgroup had all of it and has written it
-    float m = -__builtin_inff();
-    for (int b = p.b0 + tid; b <= p.b1; b += 256) m = fmaxf(m, a.slot_stats[p.slot(b) * 2]);
+    // the first parts of each wave are on their way while the statistics are looked at
+    constexpr int AHEAD = 8;
+    float ahead[AHEAD][D / 64];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (p.b0 + wave + 4 * i <= p.b1)
+#pragma unroll
+            for (int e = 0; e < D / 64; ++e) ahead[i][e] = a.slots[p.slot(p.b0 + wave + 4 * i) * D + e * 64 + lane];
+    float mine = -__builtin_inff(), l = 0.0f;            // of part b0 + tid
+    if (p.b0 + tid <= p.b1) {
+        mine = a.slot_stats[p.slot(p.b0 + tid) * 2];
+        l = a.slot_stats[p.slot(p.b0 + tid) * 2 + 1];
+    }
+    float m = mine;
+    for (int b = p.b0 + tid + 256; b <= p.b1; b += 256) m = fmaxf(m, a.slot_stats[p.slot(b) * 2]);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
     if (lane == 0) red_m[wave] = m;
     __syncthreads();
     m = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3]));
-    float l = 0.0f;
-    for (int b = p.b0 + tid; b <= p.b1; b += 256) {
+    factor[tid] = __builtin_amdgcn_exp2f(mine - m);
+    l *= factor[tid];
+    for (int b = p.b0 + tid + 256; b <= p.b1; b += 256) {
         const float f = __builtin_amdgcn_exp2f(a.slot_stats[p.slot(b) * 2] - m);
         factor[b - p.b0] = f;
         l = fmaf(a.slot_stats[p.slot(b) * 2 + 1], f, l);
@@ -591,8 +605,13 @@ __device__ void join_row(const AttendArgs &a, int groups, int row)
     __syncthreads();
     l = red_l[0] + red_l[1] + red_l[2] + red_l[3];
     float acc[D / 64] = {};
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (p.b0 + wave + 4 * i <= p.b1)
+#pragma unroll
+            for (int e = 0; e < D / 64; ++e) acc[e] = fmaf(ahead[i][e], factor[wave + 4 * i], acc[e]);
 #pragma unroll 4
-    for (int b = p.b0 + wave; b <= p.b1; b += 4) {
+    for (int b = p.b0 + wave + 4 * AHEAD; b <= p.b1; b += 4) {
         const float f = factor[b - p.b0];
 #pragma unroll
         for (int e = 0; e < D / 64; ++e) acc[e] = fmaf(a.slots[p.slot(b) * D + e * 64 + lane], f, acc[e]);
