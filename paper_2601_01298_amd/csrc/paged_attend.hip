@@ -79,6 +79,13 @@ struct Run {
     __device__ __forceinline__ void find(const AttendArgs &a, int pairs, int groups, int b)
     {
         const int lane = threadIdx.x & 63, cap = a.per_seq << a.page_shift, each = (a.S + 63) / 64;
+        if (a.S == 1) {                                  // nothing to look for: 0.5 to 1 us of a call
+            s = first = 0;
+            total = (paged_rows(as_scalar(a.len)[0], cap) + UNIT - 1) / UNIT * pairs;
+            from = share_start(total, groups, b);
+            to = share_start(total, groups, b + 1);
+            return;
+        }
         int mine = 0;
         for (int i = 0; i < each; ++i) {
             const int q = lane * each + i;
