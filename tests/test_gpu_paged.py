@@ -95,6 +95,16 @@ def test_attend_with_many_sequences(ws, dtype, S):
     lens = [int(n) for n in np.exp(rng.uniform(0, math.log(400), S)).astype(int)]
     lens[S // 2] = 0
     run_attend(ws, plain.Cache(lens, 2, 64, 16, dtype, seed=S), 2)
+    # tables of 6400 rows: the rows of all sequences are shared out over the workgroups
+    run_attend(ws, plain.Cache(lens, 2, 64, 16, dtype, seed=S, per_seq=400), 2)
+    run_attend(ws, plain.Cache(lens, 1, 128, 256, dtype, seed=S, per_seq=25), 1, weights=False)
+
+
+def test_attend_with_very_many_sequences(ws):
+    rng = np.random.default_rng(7)
+    lens = [int(n) for n in rng.integers(0, 90, 1500)]
+    run_attend(ws, plain.Cache(lens, 1, 64, 16, BF16, seed=7, per_seq=400), 3)
+    run_attend(ws, plain.Cache([0] * 1499 + [5000], 1, 64, 16, BF16, seed=7), 3)
 
 
 @pytest.mark.parametrize("dtype,d,n,H,g", [(BF16, 128, 70001, 1, 4), (BF16, 64, 40000, 2, 1), (F32, 128, 20011, 1, 2), (F32, 64, 9000, 3, 5)])
@@ -130,6 +140,24 @@ def test_attend_scale_and_equal_rows(ws):
     c.K[c.table[0].long()[r // 32], 0, r % 32] = 0.5
     O, lse, mass = run_attend(ws, c, 2, before="none")
     assert (mass[0, 0, :640] - 2.0 / 640).abs().max() <= 2.0 ** -16 * 2.0 / 640
+
+
+@pytest.mark.parametrize("lens", [[300, 41], [3000, 2999]])
+def test_attend_accounts_that_are_not_aligned(ws, lens):
+    """Accounts that start at an odd multiple of four bytes: the same bits as aligned ones."""
+    c = plain.Cache(lens, 2, 64, 16, BF16, seed=21)
+    cache = c.dev(ws)
+    Q = torch.randn((2, 6, 64), generator=c.gen).to(BF16).cuda()
+    old = torch.rand((2, 2, c.rows), generator=c.gen).cuda()
+    odd = lambda: torch.zeros(old.numel() + 1, device="cuda")[1:].view(old.shape)
+    want, got, start = torch.zeros_like(old), odd(), odd()
+    start.copy_(old)
+    assert got.data_ptr() % 16 == 4
+    ws.ws_synapse_paged_attend(cache, Q, decay=0.5, mass_in=old, mass_out=want)
+    ws.ws_synapse_paged_attend(cache, Q, decay=0.5, mass_in=start, mass_out=got)
+    assert torch.equal(got, want) and (want[0, :, :lens[0]] > 0).all()
+    with pytest.raises(ws.WsError):
+        ws.ws_synapse_paged_attend(cache, Q, O=torch.zeros(2 * 6 * 64 + 1, device="cuda")[1:].view(2, 6, 64))
 
 
 def test_attend_lengths_and_pages_out_of_range(ws):
