@@ -4,7 +4,7 @@
 // One workgroup per token.  Its d/2 angles are formed once, one per thread (position times frequency in float64, in turns, less
 // the whole turns, then the fp32 sine and cosine of half-turns), and wait in LDS for all heads of the token; then a thread
 // takes 16 bytes of the lower half of a head's row and the 16 bytes they pair with.  Bound: HBM for prompts (32768 tokens, 8 key and
-// 32 query heads of 128, bf16: 808 MB in 144 us, 5.6 TB/s of reads and writes), the launch for a decode step (100 tokens: 4.5 us).
+// 32 query heads of 128, bf16: 808 MB in 137 us, 5.9 TB/s of reads and writes), the launch for a decode step (100 tokens: 4.5 us).
 #include "paged_internal.h"
 
 namespace ws {
@@ -23,6 +23,15 @@ struct AppendArgs {
     int32_t *stamp;
     float *mass;
 };
+
+// Past the caches: a prompt is larger than they are (144 us with ordinary stores, 137 with these), and what reads a decode step's rows next
+// runs on other dies.
+__device__ __forceinline__ void store16(char *p, const uint4 &x)
+{
+    typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+    const u32x4_t v = {x.x, x.y, x.z, x.w};
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t *>(p));
+}
 
 template <bool BF16>
 __device__ __forceinline__ void rotate16(uint4 &lo, uint4 &hi, const float2 *cs)
@@ -101,14 +110,14 @@ append_tokens(AppendArgs a, RotaryTable rot)
                         : a.q_out + ((long long)t * a.Hq + (h - rotated)) * (D * ES);
         uint4 x = *reinterpret_cast<const uint4 *>(src + p * 16), y = *reinterpret_cast<const uint4 *>(src + HALF * ES + p * 16);
         if (a.pos != nullptr) rotate16<BF16>(x, y, cs + p * PER);
-        *reinterpret_cast<uint4 *>(dst + p * 16) = x;
-        *reinterpret_cast<uint4 *>(dst + HALF * ES + p * 16) = y;
+        store16(dst + p * 16, x);
+        store16(dst + HALF * ES + p * 16, y);
     }
     if (!write) return;
     for (int i = tid; i < a.H * 2 * PP; i += 256) {
         const int h = i / (2 * PP), p = i % (2 * PP);
         char *dst = reinterpret_cast<char *>(a.V) + (paged_base(page, a.pages, a.H, h, a.page) + row % a.page) * (D * ES);
-        *reinterpret_cast<uint4 *>(dst + p * 16) = *reinterpret_cast<const uint4 *>(a.v + t * a.v_token + h * a.v_head + p * 16);
+        store16(dst + p * 16, *reinterpret_cast<const uint4 *>(a.v + t * a.v_token + h * a.v_head + p * 16));
     }
     for (int h = tid; h < a.H; h += 256) {
         const long long at = ((long long)s * a.H + h) * cap + row;
