@@ -37,8 +37,8 @@ __host__ __device__ static inline int logit_rows(int cap) { return (cap + 31) / 
 static inline bool paged_logits_fit(int g, int cap) { return (long long)logit_rows(cap) * g < (1LL << 29); }
 
 // Whether every (sequence, KV head) goes to one workgroup that does all of it, in one launch.  Short caches, where the second launch costs
-// more than a few tiles one after the other (2 heads of 200 rows: 3.9 us against 9.5; 8 of 700: 12.8 against 11.6; 8 of 2000: 29.5
-// against 11.4), and so many heads that they fill the chip as they are, as long as their logits fit LDS (1600 heads of up to 1200 rows
+// more than a few tiles one after the other (2 heads of 200 rows: 3.9 us against 9.5; 8 of 700: 12.8 against 11.2; 8 of 2000: 29.5
+// against 10.7), and so many heads that they fill the chip as they are, as long as their logits fit LDS (1600 heads of up to 1200 rows
 // with weights: 68 us against 75; 512 of 4000 without: the same).
 constexpr int kWholeRows = 512, kWholePairs = 512;
 constexpr int kWholeLogits = 5120;          // 20 KB beside the merge area
