@@ -532,10 +532,14 @@ def ws_synapse_paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor,
     """k, v [T,Hkv,d] (any strides over rows) join the cache, whose len already counts them; first [S+1] int32.
     pos [axes,T] (or [T]) int32 and pairs (d/2 pairs for one axis): keys rotate, and q [T,Hq,d] into q_out, which is returned.
     stamp [S,Hkv,rows] int32 (with seen [S] int32) and mass [S,Hkv,rows] fp32 are started for the new rows."""
+    if k.dim() != 3:
+        raise ValueError("k must be [T,Hkv,d]")
     T = k.shape[0]
     krows, vrows = cache._rows(k, "k", T, cache.Hkv), cache._rows(v, "v", T, cache.Hkv)
     axes, npairs, posp = 0, None, None
     if pos is not None:
+        if pos.dim() not in (1, 2):
+            raise ValueError("pos must be [axes,T] or [T]")
         axes = 1 if pos.dim() == 1 else pos.shape[0]
         posp = cache._ptr(pos, "pos", (T,) if pos.dim() == 1 else (axes, T), torch.int32)
         pairs = tuple(pairs) if pairs is not None else (cache.d // 2,) if axes == 1 else ()
