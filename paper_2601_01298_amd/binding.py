@@ -169,8 +169,14 @@ def _check(status: int, where: str):
         raise WsError(status, where)
 
 
+def _int32(n):
+    """A number for a C int, which would keep only its low 32 bits: one that does not fit becomes the end of the range that it
+    lies beyond, which the library refuses."""
+    return max(-0x80000000, min(n, 0x7FFFFFFF))
+
+
 def ws_synapse_workspace_bytes(op: int, dt: int, H: int, L: int, d: int, k: int = 1, N: int = 1, Hq: int = 1) -> int:
-    n = lib().ws_synapse_workspace_bytes(op, dt, H, L, d, k, N, Hq)
+    n = lib().ws_synapse_workspace_bytes(op, dt, H, L, d, _int32(k), N, Hq)
     if n == ctypes.c_size_t(-1).value:
         raise WsError(WS_ERR_UNSUPPORTED, "ws_synapse_workspace_bytes")
     return int(n)
@@ -547,7 +553,7 @@ def ws_synapse_paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor,
         if npairs is None or len(pairs) != axes:
             if len(pairs) != axes:
                 raise ValueError("one number of pairs per axis")
-            npairs = cache._pairs[pairs] = (ctypes.c_int * axes)(*[int(n) for n in pairs])
+            npairs = cache._pairs[pairs] = (ctypes.c_int * axes)(*[_int32(int(n)) for n in pairs])
     qrows, Hq, qp = None, 0, None
     if q is not None:
         if q.dim() != 3:
@@ -557,7 +563,7 @@ def ws_synapse_paged_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor,
         if q_out is None:
             q_out = _new((T, Hq, cache.d), q.dtype, cache.device, stream)
         qp = cache._ptr(q_out, "q_out", (T, Hq, cache.d), cache.dtype)
-    _check(lib().ws_synapse_paged_append(cache._ref, ctypes.byref(krows), ctypes.byref(vrows), T,
+    _check(lib().ws_synapse_paged_append(cache._ref, ctypes.byref(krows), ctypes.byref(vrows), _int32(T),
                                          cache._ptr(first, "first", (cache.S + 1,), torch.int32), posp, axes, npairs, base, qrows, Hq, qp,
                                          cache._ptr(seen, "seen", cache._per_seq, torch.int32),
                                          cache._ptr(stamp, "stamp", cache._per_row, torch.int32),
@@ -596,7 +602,7 @@ def ws_synapse_paged_evict(cache: PagedCache, keep: int, seen: torch.Tensor, mas
     len_out = cache.len if len_out is None else len_out
     workspace = cache._workspace(workspace, "evict", stream, keep=keep)
     ptr, per_row = cache._ptr, cache._per_row
-    _check(lib().ws_synapse_paged_evict(cache._ref, keep, sinks, recent, ptr(seen, "seen", cache._per_seq, torch.int32),
+    _check(lib().ws_synapse_paged_evict(cache._ref, _int32(keep), _int32(sinks), _int32(recent), ptr(seen, "seen", cache._per_seq, torch.int32),
                                         ptr(mass_in, "mass_in", per_row, torch.float32), ptr(mass_out, "mass_out", per_row, torch.float32),
                                         ptr(stamp_in, "stamp_in", per_row, torch.int32), ptr(stamp_out, "stamp_out", per_row, torch.int32),
                                         ptr(len_out, "len_out", cache._per_seq, torch.int32),

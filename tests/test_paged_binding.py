@@ -38,3 +38,58 @@ def test_positions_with_another_number_of_dimensions(b, shape):
     c, good = host_cache(b), torch.zeros((3, 2, 64), dtype=torch.bfloat16)
     with pytest.raises(ValueError):
         b.ws_synapse_paged_append(c, good, good, torch.zeros((4,), dtype=torch.int32), pos=torch.zeros(shape, dtype=torch.int32))
+
+
+class Recorder:
+    """Stands in for the loaded library: keeps what a call was given and answers as told."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            return 0
+        return call
+
+
+@pytest.fixture
+def recorded(b, monkeypatch):
+    r = Recorder()
+    monkeypatch.setattr(b, "lib", lambda: r)
+    monkeypatch.setattr(b, "_device", lambda: -1)
+    monkeypatch.setattr(b, "_raw_stream", lambda device: 0)
+    return r
+
+
+@pytest.mark.parametrize("n", [2 ** 31, 2 ** 32 + 8, 2 ** 64 + 8, -2 ** 32 + 8, -2 ** 31 - 1])
+def test_numbers_of_more_than_32_bits_do_not_wrap(b, recorded, n):
+    """A ctypes int keeps the low 32 bits: 2^32 + 8 rows to keep would be 8, and the rest of the cache given up.  What reaches the
+    library is out of its range on the same side, so that it refuses the call."""
+    c = host_cache(b)
+    per_row = lambda t: torch.zeros(c._per_row, dtype=t)
+    for name in ("keep", "sinks", "recent"):
+        kw = {"keep": 8, "sinks": 0, "recent": 0, name: n}
+        b.ws_synapse_paged_evict(c, kw["keep"], torch.zeros((3,), dtype=torch.int32), per_row(torch.float32), per_row(torch.int32), sinks=kw["sinks"],
+                                 recent=kw["recent"], workspace=torch.zeros(256, dtype=torch.uint8))
+        got = dict(zip(("keep", "sinks", "recent"), recorded.calls[-1][1][1:4]))
+        assert all(-2 ** 31 <= x < 2 ** 31 for x in got.values()), got
+        assert got[name] >= 2 ** 24 if n > 0 else got[name] < 0
+        assert all(got[o] == kw[o] for o in got if o != name)
+    b.ws_synapse_workspace_bytes(b.WS_OP_PAGED_EVICT, b.WS_BF16, 2, 64, 64, k=n, N=3)
+    assert recorded.calls[-1][1][5] == (2 ** 31 - 1 if n > 0 else -2 ** 31)
+
+
+def test_more_tokens_than_32_bits_count(b, recorded):
+    c = host_cache(b)
+    k = torch.zeros((1, 2, 64), dtype=torch.bfloat16).expand(2 ** 32 + 1, 2, 64)
+    b.ws_synapse_paged_append(c, k, k, torch.zeros((4,), dtype=torch.int32))
+    T = recorded.calls[-1][1][3]
+    assert recorded.calls[-1][0] == "ws_synapse_paged_append" and 2 ** 24 <= T < 2 ** 31
+
+
+@pytest.mark.parametrize("pairs", [(2 ** 32 + 32,), (2 ** 32 + 16, -2 ** 32 + 16)])
+def test_numbers_of_pairs_do_not_wrap(b, recorded, pairs):
+    c, good = host_cache(b), torch.zeros((3, 2, 64), dtype=torch.bfloat16)
+    b.ws_synapse_paged_append(c, good, good, torch.zeros((4,), dtype=torch.int32), pos=torch.zeros((len(pairs), 3), dtype=torch.int32), pairs=pairs)
+    assert list(recorded.calls[-1][1][7]) == [2 ** 31 - 1 if n > 0 else -2 ** 31 for n in pairs]
