@@ -132,11 +132,13 @@ def _stream(stream) -> int:
 
 
 def _on_stream(stream):
-    """Context in which torch allocates for the stream the kernels will run on, so that the caching
-    allocator never hands a temporary or an output to other work while those kernels still use it."""
-    if stream is None or not hasattr(stream, "cuda_stream"):
+    """Context in which torch allocates for the stream the kernels will run on (a torch stream or a raw handle), so that
+    the caching allocator never hands a temporary or an output to other work while those kernels still use it."""
+    if stream is None:
         import contextlib
         return contextlib.nullcontext()
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream()
     return torch.cuda.stream(stream)
 
 

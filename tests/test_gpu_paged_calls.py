@@ -1,0 +1,40 @@
+"""The paged cache's calls as a program makes them: streams, sizes at the borders of the choices between kernels."""
+import pytest
+import torch
+
+import _paged as plain
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def ws():
+    from paper_2601_01298_amd import binding
+    binding.lib()
+    return binding
+
+
+def test_a_stream_given_by_its_handle(ws):
+    """The same bits as on the stream object, and the workspace that the call made for itself is not handed to the current stream while
+    the other one may still use it."""
+    c = plain.Cache([3000, 700, 0, 41], 2, 64, 16, BF16, seed=31)
+    cache = c.dev(ws)
+    Q = torch.randn((4, 6, 64), generator=c.gen).to(BF16).cuda()
+    want = ws.ws_synapse_paged_attend(cache, Q)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = ws.ws_synapse_paged_attend(cache, Q, stream=side.cuda_stream)
+    zero = ws.ws_synapse_paged_attend(cache, Q, stream=0)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(zero, want)
+    size = 37 << 20
+    w = ws._workspace(size, cache.device, None, side.cuda_stream)
+    at = w.data_ptr()
+    del w
+    here = torch.empty(size, dtype=torch.uint8, device="cuda")
+    with torch.cuda.stream(side):
+        there = torch.empty(size, dtype=torch.uint8, device="cuda")
+    assert here.data_ptr() != at and there.data_ptr() == at
+    torch.cuda.synchronize()

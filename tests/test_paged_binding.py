@@ -93,3 +93,32 @@ def test_numbers_of_pairs_do_not_wrap(b, recorded, pairs):
     c, good = host_cache(b), torch.zeros((3, 2, 64), dtype=torch.bfloat16)
     b.ws_synapse_paged_append(c, good, good, torch.zeros((4,), dtype=torch.int32), pos=torch.zeros((len(pairs), 3), dtype=torch.int32), pairs=pairs)
     assert list(recorded.calls[-1][1][7]) == [2 ** 31 - 1 if n > 0 else -2 ** 31 for n in pairs]
+
+
+def test_memory_for_a_stream_given_by_its_handle_belongs_to_that_stream(b, monkeypatch):
+    """A workspace made by the call is free again when the call returns.  Allocated on the current stream it would be given to that
+    stream's next work while the kernels on the other one still use it."""
+    entered = []
+
+    class Stream:
+        def __init__(self, handle):
+            self.cuda_stream = handle
+
+    class on:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            entered.append(self.stream.cuda_stream)
+
+        def __exit__(self, *a):
+            pass
+
+    monkeypatch.setattr(torch.cuda, "ExternalStream", Stream)
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda *a: Stream(0))
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    for make in (lambda s: b._workspace(512, "cpu", None, s), lambda s: b._new((3,), torch.float32, "cpu", s)):
+        for stream, want in ((None, []), (0x5550, [0x5550]), (0, [0]), (Stream(0x7770), [0x7770])):
+            entered.clear()
+            make(stream)
+            assert entered == want, stream
