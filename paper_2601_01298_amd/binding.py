@@ -518,7 +518,11 @@ class PagedCache:
         """The stream to enqueue on; kernels are launched on the current device, so the cache has to be there."""
         if self._index != _device():
             raise ValueError(f"the cache is on {self.device}, the current device is {torch.cuda.current_device()}")
-        return _raw_stream(self._index) if stream is None else _stream(stream)
+        if stream is None:
+            return _raw_stream(self._index)
+        if getattr(stream, "device_index", self._index) != self._index:
+            raise ValueError(f"the stream is on device {stream.device_index}, the cache on {self.device}")
+        return _stream(stream)
 
 
 def ws_synapse_paged_workspace(cache: PagedCache, op: str, Hq: int = 0, weights: bool = False, keep: int = 0, stream=None) -> torch.Tensor:

@@ -122,3 +122,18 @@ def test_memory_for_a_stream_given_by_its_handle_belongs_to_that_stream(b, monke
             entered.clear()
             make(stream)
             assert entered == want, stream
+
+
+def test_a_stream_of_another_device_is_refused(b, recorded):
+    from types import SimpleNamespace
+    c = host_cache(b)
+    good = torch.zeros((3, 2, 64), dtype=torch.bfloat16)
+    stream = lambda index: SimpleNamespace(cuda_stream=0x40, device=torch.device("cuda", index), device_index=index)
+    with pytest.raises(ValueError, match="stream"):
+        b.ws_synapse_paged_append(c, good, good, torch.zeros((4,), dtype=torch.int32), stream=stream(1))
+    assert not recorded.calls
+    c._index = 0
+    b._device = lambda: 0                                # (put back by the fixture)
+    assert c._stream(stream(0)) == 0x40
+    with pytest.raises(ValueError, match="stream"):
+        c._stream(stream(1))
