@@ -336,8 +336,10 @@ ws_status ws_synapse_inject(void *Kc, void *Vc, ws_dtype dt, int H, int Lcap, in
 /*
  * Row r of sequence s is row r % page of page table[s, r / page].  The structure lives on the host and is read during the call;
  * what it points to lives on the device.
- *   len counts what is there AFTER an append.  A value outside [0, per_seq * page] is clamped into range, a page number outside
- *   [0, pages) is not followed: an append or a move to such a page is left out, a row read from one counts as row of page 0.
+ *   len counts what is there AFTER an append.  The attention and the eviction clamp a value outside [0, per_seq * page] into that
+ *   range; the append does not, since new rows are counted back from len: rows that come to lie outside the table are left out, and of
+ *   a sequence that has outgrown its table the others see the rows that were there before.  A page number outside [0, pages) is
+ *   not followed: an append or a move to such a page is left out, a row read from one counts as row of page 0.
  *   Table entries behind a sequence's last page in use are not read.  Rows behind a sequence's last one may hold anything (NaN too).
  * A page may stand in several tables, and several times in one, as long as it is only read.
  * S * Hkv and S * Hq are at most 2^20 (WS_ERR_UNSUPPORTED beyond).
@@ -370,11 +372,13 @@ typedef struct {
  *   first      dev [S+1], first[0] = 0, not falling; tokens t >= first[S] are left out (a padded batch)
  *   pos        dev [axes, T] positions, or NULL: keys and queries are copied as they are (axes, pairs_host, base are not looked at)
  *   axes       1 to 4;  pairs_host host [axes] numbers of pairs, each >= 0, d/2 in all;  base > 0
- *   q, q_out   rows [T, Hq, d] and dev [T, Hq, d] dense, written; q NULL: keys and values only (Hq and q_out are not looked at)
+ *   q, q_out   rows [T, Hq, d] and dev [T, Hq, d] dense, 16-byte aligned, written; q NULL: keys and values only (Hq and q_out are
+ *              not looked at)
  *   stamp      dev [S, Hkv, per_seq * page] int32 or NULL: the new rows' numbers in the order of their sequence,
  *              seen[s] - n + (t - first[s]), which stay with a row when an eviction moves it
  *   seen       dev [S] tokens the sequence has had so far, this append included (len while nothing was evicted); NULL with stamp NULL
- *   mass       dev [S, Hkv, per_seq * page] fp32 or NULL: the new rows' accounts, set to 0
+ *   mass       dev [S, Hkv, per_seq * page] fp32 or NULL: the new rows' accounts, set to 0.  They grow by the attention of later tokens
+ *              only: rows of a prompt that nothing has attended to yet are equal to an eviction, which keeps the first of them
  * The page of a new row must stand in one table only, and once.  q_out may be q itself where that is dense, and overlaps nothing else.  Rows outside
  * the table are left out.
  */
@@ -389,11 +393,13 @@ ws_status ws_synapse_paged_append(const ws_paged_cache *cache, const ws_rows *k,
  *     mass_out[s,h,r] = decay * mass_in[s,h,r] + sum_{q in the g heads of h} p[q,r]                         r < len[s]
  * A sequence of no rows gives O = 0 and lse = -infinity.  The cache is split over the device by its rows, whatever their
  * sequence, and joined; the same call on the same device gives the same bits.
- *   Q dev [S, Hq, d] dtype of the cache, already rotated;  Hq % Hkv == 0;  scale <= 0 means 1/sqrt(d)
- *   O dev [S, Hq, d] fp32;  lse dev [S, Hq] fp32 or NULL;  workspace may be NULL when the reported size is 0 (short caches)
+ *   Q dev [S, Hq, d] dtype of the cache, already rotated, 16-byte aligned;  Hq % Hkv == 0;  scale <= 0 means 1/sqrt(d)
+ *   O dev [S, Hq, d] fp32, 16-byte aligned;  lse dev [S, Hq] fp32 or NULL;  workspace may be NULL when the reported size is 0 (short
+ *   caches).  Sums are fp32 and divided at the end: a logit times log2(e), and |V| times 2^8 len, have to stay within its range.
  *   mass_out dev [S, Hkv, per_seq * page] fp32 or NULL: no weights;  mass_in the same or NULL: from 0 on;  mass_in may be mass_out.
  *   Entries of rows behind len[s] are left as they are.  decay finite, >= 0 (1: a plain sum).  With weights per_seq * page * g stays
- *   below 2^29, and the workspace holds a logit per query head and row of the tables.
+ *   below 2^29, and the workspace holds a logit per query head and row of the tables, whatever is in use: 256 sequences under 32 query
+ *   heads take 0.5 GB with tables of 16384 rows, 4.3 GB with tables of 131072.
  *   The accounts are kept by sequence, not by page, so sequences that share pages have accounts of their own.
  */
 ws_status ws_synapse_paged_attend(const ws_paged_cache *cache, const void *Q, int Hq, float scale, float *O, float *lse, float decay,
@@ -411,6 +417,7 @@ ws_status ws_synapse_paged_attend(const ws_paged_cache *cache, const void *Q, in
  *   mass_out, stamp_out  the same, entries below len_out[s] written, the others left as they are; either may be its input
  *   len_out   dev [S], min(len, keep), written; may be cache->len
  *   kept      dev [S, Hkv, keep] int32 or NULL: the row each row below len_out[s] was before (entries behind left as they are)
+ * The workspace follows the tables' width: up to 16384 rows 8 bytes for each row that can move, above that 7 more for every row.
  * Rows of K and V at `keep` and behind are left as they are, so the call can be made again with the same inputs.  A page in which rows
  * move must stand in one table only, and once; rows that are protected from the first eviction on, at the head of the table, never move.
  */
