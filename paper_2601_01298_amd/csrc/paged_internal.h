@@ -38,15 +38,34 @@ static inline bool paged_logits_fit(int g, int cap) { return (long long)logit_ro
 
 // Whether every (sequence, KV head) goes to one workgroup that does all of it, in one launch.  Short caches, where the second launch costs
 // more than a few tiles one after the other (2 heads of 200 rows: 3.9 us against 9.5; 8 of 700: 12.8 against 11.2; 8 of 2000: 29.5
-// against 10.7), and so many heads that they fill the chip as they are, as long as their logits fit LDS (1600 heads of up to 1200 rows
-// with weights: 68 us against 75; 512 of 4000 without: the same).
-constexpr int kWholeRows = 512, kWholePairs = 512;
+// against 10.7), and so many heads that they fill the chip as they are, up to a width of the tables at which the longest head there
+// may be does not keep one compute unit busy long after the others: the lengths are on the device.  A row costs its workgroup 8 ns at
+// d = 64, 14 ns at 128; a batch of one long sequence among short ones ends with it.  us, one workgroup per head / equal runs, bf16 at
+// d = 128, g = 1, with all sequences as long as the table, spread evenly in their logarithm, and one that long among ones of 64 rows:
+//                                 rows   equal        log-spread   one long
+//     512 heads, no weights       1216    51 / 54      36 / 40      21 / 14
+//                                 1536    63 / 66      34 / 43      25 / 15
+//                                 2048    83 / 85      40 / 46      32 / 14
+//                                 5120   203 / 200     89 / 72      72 / 19
+//     1600 heads, no weights      1536   203 / 194     66 / 112     30 / 28
+//                                 2048   270 / 254     90 / 99      39 / 29
+//                                 5120   675 / 613    185 / 185     79 / 36
+//     512 heads, weights          1216    53 / 60      23 / 42      22 / 16
+//                                 2048    87 / 93      47 / 52      33 / 17
+//                                 2560   108 / 116     63 / 70      39 / 19
+//                                 4096   173 / 186     68 / 65      60 / 19
+//     1600 heads, weights         2048   295 / 299     84 / 146     36 / 36
+//                                 4096   593 / 597    167 / 206     65 / 42
+// (d = 64 and fp32 alike.)  Behind 1536 rows one workgroup per head gains nothing without weights.  With them, whose logits then stay in
+// LDS, it gains up to 15 % (512 heads of 4096 rows, d = 64: 88 / 104) where all are as long as their table, and takes three times as
+// long where one is.
+constexpr int kWholeRows = 512, kWholePairs = 512, kWholePairRows = 1536, kWholePairRowsWeights = 2048;
 constexpr int kWholeLogits = 5120;          // 20 KB beside the merge area
 static inline bool paged_whole_heads(int S, int Hkv, int Hq, int cap, bool weights)
 {
     const int g = Hq / Hkv;
     if (weights && (g > kPagedQueries || (long long)(logit_rows(cap) + 4) * g > kWholeLogits)) return false;
-    return cap <= kWholeRows || ((long long)S * Hkv >= kWholePairs && cap <= kWholeLogits);
+    return cap <= kWholeRows || ((long long)S * Hkv >= kWholePairs && cap <= (weights ? kWholePairRowsWeights : kWholePairRows));
 }
 
 struct PagedAttendSpace {

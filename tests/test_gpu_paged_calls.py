@@ -38,3 +38,23 @@ def test_a_stream_given_by_its_handle(ws):
         there = torch.empty(size, dtype=torch.uint8, device="cuda")
     assert here.data_ptr() != at and there.data_ptr() == at
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,weights", [(1536, False), (1552, False), (2048, True), (2064, True)])
+def test_one_long_sequence_among_short_ones(ws, dtype, rows, weights):
+    """512 heads, on both sides of the widths up to which each has a workgroup of its own."""
+    lens = [5 + i for i in range(64)]
+    lens[17], lens[40] = rows, 0
+    c = plain.Cache(lens, 8, 64, 16, dtype, seed=rows)
+    Q = torch.randn((64, 8, 64), generator=c.gen).to(dtype)
+    want = plain.attend(c, Q)
+    cache = c.dev(ws)
+    none = ws.ws_synapse_workspace_bytes(ws.WS_OP_PAGED_ATTEND, ws._dtype_code(cache.K), 8, cache.rows, 64, k=int(weights), N=64, Hq=8) == 0
+    assert none == (rows in (1536, 2048))
+    lse = torch.empty((64, 8), device="cuda")
+    mass = torch.full((64, 8, cache.rows), float("nan"), device="cuda") if weights else None
+    O = ws.ws_synapse_paged_attend(cache, Q.cuda(), lse=lse, mass_out=mass)
+    plain.check_attention(O, lse, want, rows)
+    if weights:
+        plain.check_weights(mass, None, 1.0, want, lens, rows)

@@ -137,3 +137,12 @@ def test_a_stream_of_another_device_is_refused(b, recorded):
     assert c._stream(stream(0)) == 0x40
     with pytest.raises(ValueError, match="stream"):
         c._stream(stream(1))
+
+
+def test_wide_tables_are_shared_out_however_many_heads_there_are(b):
+    """A workgroup per head (no workspace) only where the longest head there may be is short: the lengths are on the device, and one
+    head of 5000 rows among short ones would take 72 us by itself where equal runs take 19."""
+    size = lambda L, weights, N=64, H=8, Hq=8: b.ws_synapse_workspace_bytes(b.WS_OP_PAGED_ATTEND, b.WS_BF16, H, L, 128, k=weights, N=N, Hq=Hq)
+    assert size(1536, 0) == 0 < size(1552, 0) and size(5120, 0) > 0 and size(4096, 0, N=512) > 0
+    assert size(2048, 1) == 0 < size(2064, 1) and size(4096, 1) > 0
+    assert size(1536, 0, N=63) > 0 and size(1216, 1, Hq=32) == 0 < size(1536, 1, Hq=32)
