@@ -1,7 +1,7 @@
 // Attention of one new token of every sequence over its paged cache.
 //     z[q,r] = scale Q[q].K[r],  O[q] = sum_r exp(z - m) V[r] / sum_r exp(z - m)
 //
-// paged_split reads the cache once.  The rows of all (sequence, KV head) pairs are counted off in tiles of TR rows, and every
+// paged_split reads the cache once for every 16 query heads of a KV head.  The rows of all (sequence, KV head) pairs are counted off in tiles of TR rows, and every
 // workgroup takes an equal run of tiles across the borders of pairs, so that a batch of unequal lengths keeps the whole chip busy.
 // Inside its part of a pair the four waves take tiles in turn; a wave does
 //     S^T = K_tile . Q^T    (rows of the result: cache rows, columns: up to 16 query heads)
@@ -34,10 +34,20 @@ namespace {
 typedef const __attribute__((address_space(4))) int32_t *scalar_i32;
 __device__ __forceinline__ scalar_i32 as_scalar(const int32_t *p) { return (scalar_i32)(uintptr_t)p; }
 
-// The cache's rows are read once: marked as such they leave the chip's caches to everything else.
+// With up to 16 query heads per KV head the cache's rows are read once: marked as such they leave the chip's caches to everything else
+// (8 heads of 131072 rows, d = 128, bf16: 83 us against 95 with ordinary loads).  With more they are read again for the next 16, and the
+// mark would keep them from being found (32 query heads per KV head, the same rows: 131 us with it, 108 without; 100 x 8 heads of
+// 1200 rows: 176, 142; fp32, 64 query heads, 8 heads of 131072 rows: 614, 356).
+template <bool ONCE, typename T>
+__device__ __forceinline__ T load_rows(const void *p)
+{
+    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const T *>(p));
+    else return *reinterpret_cast<const T *>(p);
+}
+template <bool ONCE>
 __device__ __forceinline__ uint4 load16(const void *p)
 {
-    const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p));
+    const u32x4_t v = load_rows<ONCE, u32x4_t>(p);
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
@@ -160,7 +170,7 @@ struct alignas(16) Merge {
 // One wave's way through tiles of a (sequence, KV head, query heads).  begin() says which and asks for the first tile, run() goes through
 // them, leave() puts the wave's part into LDS; begin() of the next ones may come before leave(), so that their first tile is on its
 // way while the waves' parts are put together.
-template <bool BF16, int D, int SINK>
+template <bool BF16, int D, int SINK, bool ONCE>
 struct Sweep {
     using P = Shape<BF16, D>;
     static constexpr int TR = P::TR, RB = P::RB, HV = P::HV, NK = P::NK, C = P::C, VW = P::VW, NV = P::NV;
@@ -204,7 +214,7 @@ struct Sweep {
         for (int hf = 0; hf < HV; ++hf) {
             const char *p = reinterpret_cast<const char *>(a.K) + half_base(tile, hf, id[hf]);
 #pragma unroll
-            for (int kk = 0; kk < NK; ++kk) x.k[hf][kk] = load16(p + koff + kk * 64);
+            for (int kk = 0; kk < NK; ++kk) x.k[hf][kk] = load16<ONCE>(p + koff + kk * 64);
         }
     }
     __device__ __forceinline__ void load_v(int tile)
@@ -216,12 +226,12 @@ struct Sweep {
             for (int i = 0; i < 4; ++i) {
                 if constexpr (VW == 2) {
                     typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
-                    const u32x2_t w = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t *>(p + voff + i * RB));
+                    const u32x2_t w = load_rows<ONCE, u32x2_t>(p + voff + i * RB);
                     x.v[4 * hf + i][0] = w[0], x.v[4 * hf + i][1] = w[1];
                 } else {
 #pragma unroll
                     for (int j = 0; j < VW / 4; ++j) {
-                        const uint4 w = load16(p + voff + i * RB + 16 * j);
+                        const uint4 w = load16<ONCE>(p + voff + i * RB + 16 * j);
                         x.v[4 * hf + i][4 * j] = w.x, x.v[4 * hf + i][4 * j + 1] = w.y;
                         x.v[4 * hf + i][4 * j + 2] = w.z, x.v[4 * hf + i][4 * j + 3] = w.w;
                     }
@@ -410,7 +420,7 @@ struct Sweep {
     }
 };
 
-template <bool BF16, int D, bool WEIGHTS>
+template <bool BF16, int D, bool WEIGHTS, bool ONCE>
 __global__ void __launch_bounds__(256, 3)
 paged_split(AttendArgs a)
 {
@@ -427,7 +437,7 @@ paged_split(AttendArgs a)
     if (t0 >= t1) return;
     // ---- its parts of pairs, one after the other; a part's first tile is asked for before the one before it is put together
     const int run0 = t0;
-    Sweep<BF16, D, WEIGHTS ? kToMemory : kNowhere> w(a, nullptr, 0);
+    Sweep<BF16, D, WEIGHTS ? kToMemory : kNowhere, ONCE> w(a, nullptr, 0);
     int pair, pair0, ts;                                 // the part at t0: its pair within the sequence, the pair's first tile, its tiles
     auto begin = [&]() {
         const int n = run.template skip<TR>(a, pairs, t0);
@@ -495,7 +505,7 @@ __device__ __forceinline__ void account(const AttendArgs &a, long long at, int r
 
 // Short caches: one workgroup has all rows of its (sequence, KV head, query heads), so nothing is left to join, and the logits, kept
 // in LDS, become weights in the same launch.
-template <bool BF16, int D, bool WEIGHTS>
+template <bool BF16, int D, bool WEIGHTS, bool ONCE>
 __global__ void __launch_bounds__(256, 3)
 paged_whole(AttendArgs a, int kept_stride)
 {
@@ -514,7 +524,7 @@ paged_whole(AttendArgs a, int kept_stride)
         if (tid < gt && a.lse != nullptr) a.lse[qrow + tid] = -__builtin_inff();
         return;
     }
-    Sweep<BF16, D, WEIGHTS ? kToLds : kNowhere> w(a, kept, kept_stride);
+    Sweep<BF16, D, WEIGHTS ? kToLds : kNowhere, ONCE> w(a, kept, kept_stride);
     w.begin(s, h, q0, n, 0, (n + TR - 1) / TR);
     w.run();
     w.leave(red, gt);
@@ -717,6 +727,7 @@ hipError_t launch_paged_attend(const ws_paged_cache &c, const void *Q, int Hq, f
     a.O = O, a.lse = lse, a.mass_in = mass_in, a.mass_out = mass_out, a.decay = decay;
     a.aligned = ((reinterpret_cast<uintptr_t>(mass_in) | reinterpret_cast<uintptr_t>(mass_out)) & 15) == 0;
     const int groups = paged_groups(bf16, c.S, c.Hkv, Hq, cap, c.d);
+    const bool once = a.tiles_q == 1;
     auto go = [&](auto BF, auto DD) {
         constexpr bool B = decltype(BF)::value;
         constexpr int D = decltype(DD)::value;
@@ -724,12 +735,16 @@ hipError_t launch_paged_attend(const ws_paged_cache &c, const void *Q, int Hq, f
         if (paged_whole_heads(c.S, c.Hkv, Hq, cap, mass_out != nullptr)) {
             const dim3 heads((unsigned)(c.S * c.Hkv * a.tiles_q));
             const int stride = mass_out ? logit_rows(cap) + 4 : 0;
-            if (mass_out) hipLaunchKernelGGL((paged_whole<B, D, true>), heads, block, stride * (Hq / c.Hkv) * sizeof(float), st, a, stride);
-            else hipLaunchKernelGGL((paged_whole<B, D, false>), heads, block, 0, st, a, stride);
+            // (with accounts there are 16 query heads at most)
+            if (mass_out) hipLaunchKernelGGL((paged_whole<B, D, true, true>), heads, block, stride * (Hq / c.Hkv) * sizeof(float), st, a, stride);
+            else if (once) hipLaunchKernelGGL((paged_whole<B, D, false, true>), heads, block, 0, st, a, stride);
+            else hipLaunchKernelGGL((paged_whole<B, D, false, false>), heads, block, 0, st, a, stride);
             return hipGetLastError();
         }
-        if (mass_out) hipLaunchKernelGGL((paged_split<B, D, true>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((paged_split<B, D, false>), grid, block, 0, st, a);
+        if (mass_out && once) hipLaunchKernelGGL((paged_split<B, D, true, true>), grid, block, 0, st, a);
+        else if (mass_out) hipLaunchKernelGGL((paged_split<B, D, true, false>), grid, block, 0, st, a);
+        else if (once) hipLaunchKernelGGL((paged_split<B, D, false, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((paged_split<B, D, false, false>), grid, block, 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         // The lengths are on the device: of a long table most may be empty, and no launch is made of workgroups that find nothing to do.
