@@ -166,7 +166,13 @@ __device__ __forceinline__ void leave_row(const EvictArgs &a, int pair, int i, f
 }
 
 constexpr int kMoveRows = 4;                // rows a thread of evict_move has on their way at once
-constexpr int kInlineMoves = 128;           // moves of a head that evict_pick makes itself
+// Moves of a head that evict_pick makes itself.  us, in the same launch / in one of their own, heads of 2016 rows, bf16:
+//     moves               32           64           128          256          512
+//     2 heads, d = 64      9 / 12      10 / 13      12 / 13      12 / 13      16 / 14
+//     128 heads, d = 64   10 / 13      10 / 13      12 / 15      16 / 15      20 / 17
+//     128, d = 128        11 / 13      12 / 14      16 / 15      22 / 17      31 / 22
+//     1600, d = 128       26 / 33      37 / 42      55 / 58     103 / 104    168 / 154
+constexpr int kInlineMoves = 128;
 
 // Wave w has rows 64 KPT w and up, KPT runs of 64: the order of rows is the order of waves, runs and lanes.
 template <int THREADS, int KPT, bool MOVE>

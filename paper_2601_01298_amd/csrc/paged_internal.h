@@ -22,7 +22,9 @@ static inline long long paged_most_tiles(bool bf16, int S, int Hkv, int Hq, int 
 // One workgroup of four waves per compute unit keeps the memory busiest (8 heads of 131072 rows, d = 128: 84 us with 256, 88 with 512, 90
 // with 768; 256 heads of 32768 rows, d = 64: 309, 325, 328).  Where a tile is only 4 KB and a workgroup has few of them, two hide more of
 // the way from one head to the next (128 heads of up to 4000 rows, bf16, d = 64: 21.5 us with 256, 18.7 with 512; 72 heads of up to 4100,
-// fp32, d = 64: 17.6, 16.3; but 64 heads of 2048, d = 128: 19.4, 20.2).
+// fp32, d = 64: 17.6, 16.3; but 64 heads of 2048, d = 128: 19.4, 20.2).  fp32 at d = 128, tiles of 8 KB as bf16: 8 heads of 131072 rows 179,
+// 182; 128 heads of 2048 51, 51; 72 of up to 4100 37, 37; for 128 heads of lengths spread in their logarithm up to 16384, 89 and 78, where
+// bf16 takes 51 and 51.
 static inline int paged_groups(bool bf16, int S, int Hkv, int Hq, int cap, int d)
 {
     const long long tiles = paged_most_tiles(bf16, S, Hkv, Hq, cap), want = (tiles + 3) / 4;     // four waves, a tile each
@@ -91,7 +93,13 @@ static inline size_t paged_attend_workspace_bytes(bool bf16, int S, int Hkv, int
 
 // Per KV head of a sequence: how many rows move, and from where to where.
 static inline int paged_evict_moves(int cap, int keep) { return keep >= cap ? 1 : (keep < cap - keep ? keep : cap - keep); }
-constexpr int kPickRows = 16384;            // rows of a head whose choice one workgroup makes
+// Rows of a head whose choice one workgroup makes: as many as its registers hold.  us, so / by workgroups of kChunk rows, bf16, d = 64, to
+// half and to 97 % of the rows:
+//     heads        2                         16                        128                       1600
+//     2048 rows    14 / 27,  10 / 25         15 / 27,  11 / 26         18 / 33,  11 / 28         106 / 168,  27 / 100
+//     8192         16 / 27,  18 / 28         18 / 29,  18 / 28         45 / 58,  20 / 36         472 / 512, 145 / 228
+//     16384        24 / 28,  25 / 29         29 / 33,  26 / 31         81 / 93,  33 / 48         946 / 1026, 295 / 463
+constexpr int kPickRows = 16384;
 constexpr int kChunk = 4096;                // rows per workgroup of longer ones
 // (one more than the rows fill, because no chunk has rows on both sides of `keep`)
 static inline int paged_evict_chunks(int cap) { return cap <= kPickRows ? 0 : (cap + kChunk - 1) / kChunk + 1; }
