@@ -11,8 +11,8 @@
 // rows within a contraction is free as long as V is fetched in the same one.  A lane's block of V is rows x head dimensions, which
 // the product wants the other way round; eight rows of bf16 are turned in registers by one byte permutation per pair.  Nothing of K, V
 // or P goes through LDS.  Bound: HBM (g flop per byte against 250): 8 heads of 131072 rows, d = 128, bf16: 537 MB in 80 us, 6.7 TB/s, matrix
-// cores 8 % busy.  With weights, 256 heads of 32768 rows under 8 query heads each: 4.6 GB in 874 us, 5.3 TB/s; the logits, 6 % of the
-// bytes, cost 267 us, because they are written to HBM in between the reads.
+// cores 8 % busy.  With weights, 256 heads of 32768 rows under 8 query heads each: 4.6 GB in 879 us, 5.2 TB/s; the logits, 6 % of the
+// bytes, cost 261 us, because they are written to HBM in between the reads (10 of it with all stores on a kilobyte per head).
 //
 // paged_join brings the parts of a pair that several workgroups shared to their common maximum; paged_weights adds the rows'
 // weights, from the logits that paged_split left, to their accounts.  Logits and maxima are in units of log2.
