@@ -1,8 +1,9 @@
 // Attention of one new token of every sequence over its paged cache.
 //     z[q,r] = scale Q[q].K[r],  O[q] = sum_r exp(z - m) V[r] / sum_r exp(z - m)
 //
-// paged_split reads the cache once for every 16 query heads of a KV head.  The rows of all (sequence, KV head) pairs are counted off in tiles of TR rows, and every
-// workgroup takes an equal run of tiles across the borders of pairs, so that a batch of unequal lengths keeps the whole chip busy.
+// paged_split reads the cache once for every 16 query heads of a KV head.  The rows of all (sequence, KV head) pairs are counted off in
+// tiles of TR rows, and every workgroup takes an equal run of tiles across the borders of pairs, so that a batch of unequal lengths
+// keeps the whole chip busy.
 // Inside its part of a pair the four waves take tiles in turn; a wave does
 //     S^T = K_tile . Q^T    (rows of the result: cache rows, columns: up to 16 query heads)
 //     O^T += V_tile^T . P^T (rows: head dimensions, columns: query heads)
